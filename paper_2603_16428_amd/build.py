@@ -2,8 +2,8 @@
 
     python -m paper_2603_16428_amd.build
 
-compiles csrc/lce_api.hip (which includes the kernels) and csrc/host_adam.cpp (the host optimizer
-step) into liblce.so next to this file.
+compiles csrc/lce_api.hip (which includes the step's kernels), csrc/ops_api.hip (the operators around
+the step) and csrc/host_adam.cpp (the host optimizer step) into liblce.so next to this file.
 """
 from __future__ import annotations
 
@@ -16,8 +16,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "liblce.so")
 KERNEL_SOURCES = [os.path.join(HERE, "csrc", "lce_api.hip")]
+OPS_SOURCES = [os.path.join(HERE, "csrc", "ops_api.hip")]
 HOST_SOURCES = [os.path.join(HERE, "csrc", "host_adam.cpp")]
-SOURCES = KERNEL_SOURCES + HOST_SOURCES
+SOURCES = KERNEL_SOURCES + OPS_SOURCES + HOST_SOURCES
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [
@@ -38,19 +39,23 @@ def build(verbose: bool = False) -> str:
     """Compile liblce.so (always) and return its path. Raises on failure."""
     tmp = LIB + ".tmp"
     with tempfile.TemporaryDirectory() as d:
-        objs = []
-        for src in HOST_SOURCES:
+        # One compiler process per source, at the same time.
+        device = [HIPCC] + [f for f in FLAGS if f != "-shared"]
+        objs, started = [], []
+        for src in SOURCES:
             obj = os.path.join(d, os.path.splitext(os.path.basename(src))[0] + ".o")
-            r = subprocess.run([HOSTCXX] + HOST_FLAGS + ["-c", src, "-o", obj], capture_output=True, text=True)
-            if r.returncode != 0:
-                raise RuntimeError(f"{HOSTCXX} failed on {src}:\n" + r.stdout + r.stderr)
             objs.append(obj)
-        # Objects first: hipcc's language flag for the .hip sources applies to the inputs after it.
-        cmd = [HIPCC] + FLAGS + objs + KERNEL_SOURCES + ["-pthread", "-o", tmp]
-        r = subprocess.run(cmd, capture_output=True, text=True)
-    msgs = [ln for ln in (r.stdout + r.stderr).splitlines() if "packed-fp32-ops" not in ln]
-    if r.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + "\n".join(msgs))
+            cmd = ([HOSTCXX] + HOST_FLAGS if src in HOST_SOURCES else device) + ["-c", src, "-o", obj]
+            started.append((cmd, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+        ended = [(cmd, p.communicate()[0], p.returncode) for cmd, p in started]
+        if all(rc == 0 for _, _, rc in ended):
+            cmd = [HIPCC] + FLAGS + objs + ["-pthread", "-o", tmp]
+            r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+            ended.append((cmd, r.stdout, r.returncode))
+    msgs = [ln for _, out, _ in ended for ln in out.splitlines() if "packed-fp32-ops" not in ln]
+    failed = [" ".join(cmd) for cmd, _, rc in ended if rc != 0]
+    if failed:
+        raise RuntimeError("failed: " + "; ".join(failed) + "\n" + "\n".join(msgs))
     if verbose and msgs:
         print("\n".join(msgs), file=sys.stderr)
     os.replace(tmp, LIB)

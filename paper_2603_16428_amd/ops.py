@@ -1,0 +1,383 @@
+"""Python binding of the operators around the output-layer step (include/lce_ops.h).
+
+In front of the step: the residual's addition with the RMSNorm of the sum, with rows in their own type
+or in 8 bits with scales, and its backward. Behind it: the global norm of many gradients, and clipping
+by it. Argument marshalling only, as in lce.py: every computation runs in liblce.so's HIP kernels, on
+the current stream of the tensors' device, and nothing waits for the GPU.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from .lce import DTYPES, LCE_OK, LCEError, _bytes_are_values, load_library
+
+EXPORTED = ("lce_add_rmsnorm_forward", "lce_add_rmsnorm_quant", "lce_add_rmsnorm_workspace_size",
+            "lce_add_rmsnorm_backward", "lce_grad_norm_workspace_size", "lce_grad_norm", "lce_clip_grad_norm")
+FP8 = torch.float8_e4m3fn
+GROUP_SIZES = (0, 32, 64, 128)
+NORM_TYPES = {2.0: 0, float("inf"): 1}
+
+_lib = None
+
+
+def _library() -> ctypes.CDLL:
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = load_library()
+    i64, vp, sz, ci, f32 = ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
+    rows = [vp, i64, vp, i64, vp, i64, i64, ci, f32]
+    for name, args, res in [
+            ("lce_add_rmsnorm_forward", rows + [vp, i64, vp, i64, vp, vp], ci),
+            ("lce_add_rmsnorm_quant", rows + [ci, vp, i64, vp, vp, i64, vp, vp], ci),
+            ("lce_add_rmsnorm_workspace_size", [i64, i64, ci], sz),
+            ("lce_add_rmsnorm_backward", [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, ci, vp, i64, vp, vp, sz, vp], ci),
+            ("lce_grad_norm_workspace_size", [i64], sz),
+            ("lce_grad_norm", [vp, i64, ci, vp, vp, sz, vp], ci),
+            ("lce_clip_grad_norm", [vp, i64, ci, f32, vp, vp, vp, sz, vp], ci)]:
+        f = getattr(lib, name)
+        f.argtypes, f.restype = args, res
+    _lib = lib
+    return lib
+
+
+def _call(name: str, device, *args) -> None:
+    """A library call on the current stream of `device`, with that device the current one."""
+    f = getattr(_library(), name)
+    if device.index == torch.cuda.current_device():
+        st = f(*args, torch.cuda.current_stream(device).cuda_stream)
+    else:
+        with torch.cuda.device(device):
+            st = f(*args, torch.cuda.current_stream(device).cuda_stream)
+    if st != LCE_OK:
+        raise LCEError(st, name)
+
+
+# ---- the residual's addition and the RMSNorm of the sum --------------------------------------------
+
+def _pitch(t, what: str) -> int:
+    """Elements between the rows [N, H] that t's leading dimensions make up, its last one being H."""
+    if t.is_contiguous():
+        return t.shape[-1]
+    if t.is_neg():
+        raise ValueError(f"{what} is a lazily negated view: resolve_neg() it first")
+    shape, stride = t.shape, t.stride()
+    if shape[-1] > 1 and stride[-1] != 1:
+        raise ValueError(f"{what}: the values of a row must be consecutive")
+    pitch = span = None
+    for n, st in zip(reversed(shape[:-1]), reversed(stride[:-1])):
+        if n == 1:
+            continue
+        if pitch is None:
+            pitch = st
+        elif st != span:
+            raise ValueError(f"{what}: the rows must be evenly spaced over the leading dimensions")
+        span = n * st
+    return shape[-1] if pitch is None else pitch
+
+
+def _optional(t, what: str):
+    """Pointer and pitch of rows that may be absent."""
+    return (None, 0) if t is None else (t.data_ptr(), _pitch(t, what))
+
+
+def _check_rows(hidden, gamma):
+    if not (isinstance(hidden, torch.Tensor) and hidden.is_cuda):
+        raise ValueError("hidden must be a device tensor")
+    if hidden.dtype not in DTYPES:
+        raise ValueError("hidden must be bfloat16, float16 or float32")
+    if hidden.dim() < 1 or hidden.shape[-1] < 1:
+        raise ValueError("hidden must be [..., H]")
+    if gamma.shape != hidden.shape[-1:] or gamma.dtype != hidden.dtype or gamma.device != hidden.device:
+        raise ValueError("gamma must be [H] of the hidden dtype, on the hidden's device")
+    if not gamma.is_contiguous() or gamma.is_neg() or hidden.is_neg():
+        raise ValueError("gamma must be contiguous, and nothing a lazily negated view")
+    H = hidden.shape[-1]
+    return hidden.numel() // H, H
+
+
+def _check_like(t, hidden, what: str):
+    if t.shape != hidden.shape or t.dtype != hidden.dtype or t.device != hidden.device:
+        raise ValueError(f"{what} must have the hidden's shape, dtype and device")
+
+
+def _written(tensors) -> None:
+    """Tells autograd that the kernels write these tensors (a saved one of them is then refused in a backward)."""
+    try:
+        torch.autograd.graph.increment_version(tensors)
+    except RuntimeError:  # inference tensors have no version
+        torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
+
+
+def _output(t, like, what: str, dtype=None):
+    """A given output, checked, or a new one."""
+    if t is None:
+        return torch.empty(like.shape, dtype=dtype or like.dtype, device=like.device)
+    if t.shape != like.shape or t.dtype != (dtype or like.dtype) or t.device != like.device:
+        raise ValueError(f"{what} must have the hidden's shape and device and dtype {dtype or like.dtype}")
+    _written([t])
+    return t
+
+
+def _run_forward(hidden, residual, gamma, eps, quant, group_size, normed, added, return_rstd):
+    N, H = _check_rows(hidden, gamma)
+    dev = hidden.device
+    out = _output(normed, hidden, "normed", FP8 if quant else None)
+    scales = None
+    if quant:
+        groups = -(-H // group_size) if group_size else 1
+        scales = torch.empty(hidden.shape[:-1] + (groups,), dtype=torch.float32, device=dev)
+    if residual is None:
+        if added is not None:
+            raise ValueError("without a residual there is no sum: it is hidden itself")
+        total = hidden
+    else:
+        _check_like(residual, hidden, "residual")
+        if residual.is_neg():
+            raise ValueError("residual is a lazily negated view: resolve_neg() it first")
+        total = _output(added, hidden, "added")
+    rstd = torch.empty(hidden.shape[:-1], dtype=torch.float32, device=dev) if return_rstd else None
+    if N:
+        rows = (hidden.data_ptr(), _pitch(hidden, "hidden"), *_optional(residual, "residual"), gamma.data_ptr(), N, H,
+                DTYPES[hidden.dtype], eps)
+        sums = _optional(None if residual is None else total, "added")
+        r = None if rstd is None else rstd.data_ptr()
+        if quant:
+            _call("lce_add_rmsnorm_quant", dev, *rows, group_size, out.data_ptr(), _pitch(out, "normed"),
+                  scales.data_ptr(), *sums, r)
+        else:
+            _call("lce_add_rmsnorm_forward", dev, *rows, out.data_ptr(), _pitch(out, "normed"), *sums, r)
+    outs = (out, scales, total) if quant else (out, total)
+    return outs + (rstd,) if return_rstd else outs
+
+
+def add_rmsnorm_forward(hidden, residual, gamma, eps: float = 1e-5, normed=None, added=None,
+                        return_rstd: bool = False):
+    """(normed, added[, rstd]): added = hidden + residual and normed = RMSNorm(added) * gamma.
+
+    hidden [..., H] and residual (or None: added is hidden itself) need consecutive values in a row and
+    evenly spaced rows, not contiguity. The sum is normalised in fp32, before its rounding. `normed` and
+    `added` may be given, and may be hidden or residual themselves (a residual stream updated in place).
+    rstd [...] (fp32) is 1 / sqrt(mean(added^2) + eps), for add_rmsnorm_backward. Not differentiable: see
+    add_rmsnorm.
+    """
+    return _run_forward(hidden, residual, gamma, eps, False, 0, normed, added, return_rstd)
+
+
+def add_rmsnorm_quant(hidden, residual, gamma, eps: float = 1e-5, group_size: int = 0, quantised=None, added=None,
+                      return_rstd: bool = False):
+    """(quantised, scales, added[, rstd]): as add_rmsnorm_forward, the normalised rows as float8_e4m3fn.
+
+    Each group of `group_size` (32, 64 or 128; 0: the whole row) consecutive values of a row has one fp32
+    scale, its largest magnitude / 448: quantised * scale stands for the value. scales is
+    [..., ceil(H / group_size)] ([..., 1] with a scale per row).
+    """
+    if group_size not in GROUP_SIZES:
+        raise ValueError(f"group_size must be one of {GROUP_SIZES}")
+    return _run_forward(hidden, residual, gamma, eps, True, group_size, quantised, added, return_rstd)
+
+
+def add_rmsnorm_workspace_size(N: int, H: int, dtype=torch.bfloat16) -> int:
+    return int(_library().lce_add_rmsnorm_workspace_size(N, H, DTYPES[dtype]))
+
+
+def add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd, need_gamma: bool = True,
+                         grad_hidden=None, workspace: torch.Tensor | None = None):
+    """(grad_hidden, grad_gamma) from the upstream gradients of normed and of added (None: there is none).
+
+    hidden, residual (or None) and gamma as the forward call had them; or added and None, where one tensor
+    is kept instead of two (the sum then enters with its rounding). grad_hidden is the gradient of hidden
+    and of the residual alike; it may be given, and may be grad_normed, grad_added, hidden or residual
+    themselves. grad_gamma is None without need_gamma.
+    """
+    N, H = _check_rows(hidden, gamma)
+    dev = hidden.device
+    for t, what in ((grad_normed, "grad_normed"), (grad_added, "grad_added"), (residual, "residual")):
+        if t is not None:
+            _check_like(t, hidden, what)
+            if t.is_neg():
+                raise ValueError(f"{what} is a lazily negated view: resolve_neg() it first")
+    if rstd.shape != hidden.shape[:-1] or rstd.dtype != torch.float32 or rstd.device != dev or not rstd.is_contiguous():
+        raise ValueError("rstd must be the forward call's")
+    dx = _output(grad_hidden, hidden, "grad_hidden")
+    dg = torch.empty_like(gamma) if need_gamma else None
+    if N or need_gamma:
+        ws = None
+        if need_gamma:
+            need = _library().lce_add_rmsnorm_workspace_size(N, H, DTYPES[hidden.dtype])
+            if need == 0:
+                raise LCEError(2, "lce_add_rmsnorm_workspace_size")
+            ws = workspace if workspace is not None else torch.empty(need, dtype=torch.uint8, device=dev)
+        _call("lce_add_rmsnorm_backward", dev, grad_normed.data_ptr(), _pitch(grad_normed, "grad_normed"),
+              *_optional(grad_added, "grad_added"), hidden.data_ptr(), _pitch(hidden, "hidden"),
+              *_optional(residual, "residual"), gamma.data_ptr(), rstd.data_ptr(), N, H, DTYPES[hidden.dtype],
+              dx.data_ptr(), _pitch(dx, "grad_hidden"), None if dg is None else dg.data_ptr(),
+              None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())
+    return dx, dg
+
+
+def _upstream(g):
+    """An upstream gradient as rows that the kernels can read: its values in memory, its rows evenly spaced."""
+    if g is None:
+        return None
+    if not _bytes_are_values(g):
+        if type(g) is not torch.Tensor:
+            raise ValueError("the upstream gradient must be a plain tensor")
+        # Lazily negated or zero tensors become memory; batched ones (is_grads_batched) cannot.
+        g = torch.zeros(g.shape, dtype=g.dtype, device=g.device).add_(g)
+        if not _bytes_are_values(g):
+            raise ValueError("the upstream gradient must be a plain tensor")
+    try:
+        _pitch(g, "grad")
+        return g
+    except ValueError:
+        return g.contiguous()
+
+
+class AddRMSNorm(torch.autograd.Function):
+    """(normed, added) of add_rmsnorm_forward with its gradients; without a residual, normed alone.
+
+    The backward takes the unrounded sum, as the forward did: both addends are kept for it, not their
+    rounded sum, which would put a second rounding into every gradient (gamma's 1.5 times as far off).
+    """
+
+    @staticmethod
+    def forward(ctx, hidden, residual, gamma, eps):
+        ctx.set_materialize_grads(False)
+        need = any(ctx.needs_input_grad)
+        normed, added, *rstd = _run_forward(hidden, residual, gamma, eps, False, 0, None, None, need)
+        if need:
+            ctx.save_for_backward(hidden, residual, gamma, rstd[0])
+        return normed if residual is None else (normed, added)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_normed, grad_added=None):
+        hidden, residual, gamma, rstd = ctx.saved_tensors
+        need_gamma = ctx.needs_input_grad[2]
+        grad_normed, grad_added = _upstream(grad_normed), _upstream(grad_added)
+        if grad_normed is None:  # nothing came back through the norm
+            grads = grad_added, torch.zeros_like(gamma) if need_gamma else None
+        else:
+            grads = add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd, need_gamma)
+        need = ctx.needs_input_grad
+        return grads[0] if need[0] else None, grads[0] if need[1] else None, grads[1], None
+
+
+def add_rmsnorm(hidden, residual, gamma, eps: float = 1e-5):
+    """(normed, added): added = hidden + residual, normed = RMSNorm(added) * gamma. Differentiable (once)."""
+    if residual is None:
+        raise ValueError("residual is None: rmsnorm(hidden, gamma, eps) is the norm alone")
+    return AddRMSNorm.apply(hidden, residual, gamma, eps)
+
+
+def rmsnorm(hidden, gamma, eps: float = 1e-5):
+    """RMSNorm(hidden) * gamma over the last dimension. Differentiable (once)."""
+    return AddRMSNorm.apply(hidden, None, gamma, eps)
+
+
+# ---- the global norm of many gradients, and clipping -----------------------------------------------
+
+def _dense(t) -> bool:
+    """Whether t's values fill one block of memory, each place once, in whatever order of dimensions."""
+    if t.is_contiguous():
+        return True
+    want = 1
+    for st, n in sorted((st, n) for n, st in zip(t.shape, t.stride()) if n != 1):
+        if st != want:
+            return False
+        want *= n
+    return True
+
+
+def _check_grads(grads):
+    grads = [grads] if isinstance(grads, torch.Tensor) else [g for g in grads if g is not None]
+    if not grads:
+        raise ValueError("no gradients")
+    dev = grads[0].device
+    for g in grads:
+        if not g.is_cuda or g.device != dev:
+            raise ValueError("gradients must be tensors of one device")
+        if g.dtype not in DTYPES or g.layout != torch.strided:
+            raise ValueError("gradients must be dense bfloat16, float16 or float32 tensors")
+        if not (g.is_contiguous() or g.numel() == 0 or _dense(g)):
+            raise ValueError("a gradient's values must fill one block of memory, in any order")
+    return grads, dev
+
+
+def _table(grads):
+    """lce_tensor_t entries."""
+    flat = [v for g in grads for v in (g.data_ptr(), g.numel(), DTYPES[g.dtype])]
+    return (ctypes.c_int64 * len(flat))(*flat)
+
+
+def _norm_type(norm_type):
+    if norm_type not in NORM_TYPES:
+        raise ValueError("norm_type must be 2.0 or inf")
+    return NORM_TYPES[norm_type]
+
+
+def grad_norm_workspace_size(count: int) -> int:
+    """Bytes of workspace for `count` gradients."""
+    return int(_library().lce_grad_norm_workspace_size(count))
+
+
+def _grad_workspace(workspace, count, dev):
+    if workspace is not None:
+        return workspace
+    return torch.empty(_library().lce_grad_norm_workspace_size(count), dtype=torch.uint8, device=dev)
+
+
+def grad_norm(grads, norm_type: float = 2.0, workspace: torch.Tensor | None = None):
+    """The norm (2 or inf) over all values of the gradients: a device scalar in fp32, squares summed in fp64.
+
+    grads: device tensors (Nones among them are left out) of one device and any of the three types, each
+    filling one block of memory.
+    """
+    kind = _norm_type(norm_type)
+    grads, dev = _check_grads(grads)
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    ws = _grad_workspace(workspace, len(grads), dev)
+    _call("lce_grad_norm", dev, _table(grads), len(grads), kind, norm.data_ptr(), ws.data_ptr(), ws.numel())
+    return norm
+
+
+def _clip(grads, dev, max_norm, norm_type, out, workspace):
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    ws = _grad_workspace(workspace, len(grads), dev)
+    outs = None if out is None else (ctypes.c_void_p * len(out))(*[t.data_ptr() for t in out])
+    _written(grads if out is None else out)
+    _call("lce_clip_grad_norm", dev, _table(grads), len(grads), norm_type, max_norm, outs, norm.data_ptr(),
+          ws.data_ptr(), ws.numel())
+    return norm
+
+
+def clip_grad_norm_(grads, max_norm: float, norm_type: float = 2.0, workspace: torch.Tensor | None = None):
+    """Scales the gradients in place so that their norm is at most max_norm; returns the norm before.
+
+    The factor is min(1, max_norm / (norm + 1e-6)). Nothing waits for the norm: it and the factor stay on
+    the device, and gradients within the limit are not written. A NaN among the gradients makes all NaN.
+    """
+    kind = _norm_type(norm_type)
+    grads, dev = _check_grads(grads)
+    return _clip(grads, dev, max_norm, kind, None, workspace)
+
+
+def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, out=None, workspace: torch.Tensor | None = None):
+    """(norm, clipped): as clip_grad_norm_, with the scaled gradients in other memory.
+
+    out: tensors of the gradients' shapes, strides and types (for instance those that a copy to the host
+    reads), one for each gradient that is not None; new ones by default.
+    """
+    kind = _norm_type(norm_type)
+    grads, dev = _check_grads(grads)
+    if out is None:
+        out = [torch.empty_like(g) for g in grads]
+    else:
+        out = [out] if isinstance(out, torch.Tensor) else [t for t in out if t is not None]
+        if len(out) != len(grads) or any(t.shape != g.shape or t.dtype != g.dtype or t.device != dev
+                                         or (t.stride() != g.stride() and t.numel() > 1) for t, g in zip(out, grads)):
+            raise ValueError("out must match the gradients in number, shape, strides, dtype and device")
+    return _clip(grads, dev, max_norm, kind, out, workspace), out
