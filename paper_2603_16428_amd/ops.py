@@ -43,14 +43,21 @@ def _library() -> ctypes.CDLL:
     return lib
 
 
+# The current device and a device's current stream, as numbers. torch's public calls wrap them in objects: 5 us of
+# a call whose launch takes 4.
+_device_index = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def _call(name: str, device, *args) -> None:
     """A library call on the current stream of `device`, with that device the current one."""
-    f = getattr(_library(), name)
-    if device.index == torch.cuda.current_device():
-        st = f(*args, torch.cuda.current_stream(device).cuda_stream)
+    f = getattr(_lib or _library(), name)
+    index = device.index
+    if index == _device_index():
+        st = f(*args, _raw_stream(index))
     else:
         with torch.cuda.device(device):
-            st = f(*args, torch.cuda.current_stream(device).cuda_stream)
+            st = f(*args, _raw_stream(index))
     if st != LCE_OK:
         raise LCEError(st, name)
 
@@ -84,23 +91,27 @@ def _optional(t, what: str):
 
 
 def _check_rows(hidden, gamma):
-    if not (isinstance(hidden, torch.Tensor) and hidden.is_cuda):
+    """(N, H, device, shape) of rows and their gain."""
+    if not hidden.is_cuda:
         raise ValueError("hidden must be a device tensor")
-    if hidden.dtype not in DTYPES:
+    shape, dtype, dev = hidden.shape, hidden.dtype, hidden.device
+    if dtype not in DTYPES:
         raise ValueError("hidden must be bfloat16, float16 or float32")
-    if hidden.dim() < 1 or hidden.shape[-1] < 1:
+    if not shape or shape[-1] < 1:
         raise ValueError("hidden must be [..., H]")
-    if gamma.shape != hidden.shape[-1:] or gamma.dtype != hidden.dtype or gamma.device != hidden.device:
+    H = shape[-1]
+    if gamma.shape != (H,) or gamma.dtype != dtype or gamma.device != dev:
         raise ValueError("gamma must be [H] of the hidden dtype, on the hidden's device")
     if not gamma.is_contiguous() or gamma.is_neg() or hidden.is_neg():
         raise ValueError("gamma must be contiguous, and nothing a lazily negated view")
-    H = hidden.shape[-1]
-    return hidden.numel() // H, H
+    return hidden.numel() // H, H, dev, shape
 
 
 def _check_like(t, hidden, what: str):
     if t.shape != hidden.shape or t.dtype != hidden.dtype or t.device != hidden.device:
         raise ValueError(f"{what} must have the hidden's shape, dtype and device")
+    if t.is_neg():
+        raise ValueError(f"{what} is a lazily negated view: resolve_neg() it first")
 
 
 def _written(tensors) -> None:
@@ -114,7 +125,7 @@ def _written(tensors) -> None:
 def _output(t, like, what: str, dtype=None):
     """A given output, checked, or a new one."""
     if t is None:
-        return torch.empty(like.shape, dtype=dtype or like.dtype, device=like.device)
+        return like.new_empty(like.shape, dtype=dtype)
     if t.shape != like.shape or t.dtype != (dtype or like.dtype) or t.device != like.device:
         raise ValueError(f"{what} must have the hidden's shape and device and dtype {dtype or like.dtype}")
     _written([t])
@@ -122,23 +133,19 @@ def _output(t, like, what: str, dtype=None):
 
 
 def _run_forward(hidden, residual, gamma, eps, quant, group_size, normed, added, return_rstd):
-    N, H = _check_rows(hidden, gamma)
-    dev = hidden.device
+    N, H, dev, shape = _check_rows(hidden, gamma)
     out = _output(normed, hidden, "normed", FP8 if quant else None)
     scales = None
     if quant:
-        groups = -(-H // group_size) if group_size else 1
-        scales = torch.empty(hidden.shape[:-1] + (groups,), dtype=torch.float32, device=dev)
+        scales = hidden.new_empty(shape[:-1] + (-(-H // group_size) if group_size else 1,), dtype=torch.float32)
     if residual is None:
         if added is not None:
             raise ValueError("without a residual there is no sum: it is hidden itself")
         total = hidden
     else:
         _check_like(residual, hidden, "residual")
-        if residual.is_neg():
-            raise ValueError("residual is a lazily negated view: resolve_neg() it first")
         total = _output(added, hidden, "added")
-    rstd = torch.empty(hidden.shape[:-1], dtype=torch.float32, device=dev) if return_rstd else None
+    rstd = hidden.new_empty(shape[:-1], dtype=torch.float32) if return_rstd else None
     if N:
         rows = (hidden.data_ptr(), _pitch(hidden, "hidden"), *_optional(residual, "residual"), gamma.data_ptr(), N, H,
                 DTYPES[hidden.dtype], eps)
@@ -192,24 +199,23 @@ def add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd,
     and of the residual alike; it may be given, and may be grad_normed, grad_added, hidden or residual
     themselves. grad_gamma is None without need_gamma.
     """
-    N, H = _check_rows(hidden, gamma)
-    dev = hidden.device
-    for t, what in ((grad_normed, "grad_normed"), (grad_added, "grad_added"), (residual, "residual")):
-        if t is not None:
-            _check_like(t, hidden, what)
-            if t.is_neg():
-                raise ValueError(f"{what} is a lazily negated view: resolve_neg() it first")
-    if rstd.shape != hidden.shape[:-1] or rstd.dtype != torch.float32 or rstd.device != dev or not rstd.is_contiguous():
+    N, H, dev, shape = _check_rows(hidden, gamma)
+    _check_like(grad_normed, hidden, "grad_normed")
+    if grad_added is not None:
+        _check_like(grad_added, hidden, "grad_added")
+    if residual is not None:
+        _check_like(residual, hidden, "residual")
+    if rstd.shape != shape[:-1] or rstd.dtype != torch.float32 or rstd.device != dev or not rstd.is_contiguous():
         raise ValueError("rstd must be the forward call's")
     dx = _output(grad_hidden, hidden, "grad_hidden")
     dg = torch.empty_like(gamma) if need_gamma else None
     if N or need_gamma:
         ws = None
         if need_gamma:
-            need = _library().lce_add_rmsnorm_workspace_size(N, H, DTYPES[hidden.dtype])
+            need = (_lib or _library()).lce_add_rmsnorm_workspace_size(N, H, DTYPES[hidden.dtype])
             if need == 0:
                 raise LCEError(2, "lce_add_rmsnorm_workspace_size")
-            ws = workspace if workspace is not None else torch.empty(need, dtype=torch.uint8, device=dev)
+            ws = workspace if workspace is not None else hidden.new_empty(need, dtype=torch.uint8)
         _call("lce_add_rmsnorm_backward", dev, grad_normed.data_ptr(), _pitch(grad_normed, "grad_normed"),
               *_optional(grad_added, "grad_added"), hidden.data_ptr(), _pitch(hidden, "hidden"),
               *_optional(residual, "residual"), gamma.data_ptr(), rstd.data_ptr(), N, H, DTYPES[hidden.dtype],
@@ -246,15 +252,21 @@ class AddRMSNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, residual, gamma, eps):
         ctx.set_materialize_grads(False)
-        need = any(ctx.needs_input_grad)
+        need = True in ctx.needs_input_grad
         normed, added, *rstd = _run_forward(hidden, residual, gamma, eps, False, 0, None, None, need)
         if need:
             ctx.save_for_backward(hidden, residual, gamma, rstd[0])
         return normed if residual is None else (normed, added)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_normed, grad_added=None):
+        # Under create_graph the gradients say so if they are differentiated again; without, that costs nothing.
+        if torch.is_grad_enabled():
+            return AddRMSNorm._once(ctx, grad_normed, grad_added)
+        return AddRMSNorm._gradients(ctx, grad_normed, grad_added)
+
+    @staticmethod
+    def _gradients(ctx, grad_normed, grad_added):
         hidden, residual, gamma, rstd = ctx.saved_tensors
         need_gamma = ctx.needs_input_grad[2]
         grad_normed, grad_added = _upstream(grad_normed), _upstream(grad_added)
@@ -264,6 +276,8 @@ class AddRMSNorm(torch.autograd.Function):
             grads = add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd, need_gamma)
         need = ctx.needs_input_grad
         return grads[0] if need[0] else None, grads[0] if need[1] else None, grads[1], None
+
+    _once = staticmethod(torch.autograd.function.once_differentiable(_gradients.__func__))
 
 
 def add_rmsnorm(hidden, residual, gamma, eps: float = 1e-5):
