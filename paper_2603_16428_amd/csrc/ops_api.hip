@@ -95,13 +95,16 @@ constexpr int threads_of(int tpr) { return tpr < 256 ? 256 : tpr; }
 // Workgroups of the forward: one per group of rows (the kernel walks on where a grid that large is not
 // allowed).
 constexpr int64_t kForwardBlocks = int64_t(1) << 20;
-// Workgroups of the backward, each of which leaves H fp32 sums for dgamma.
+// Workgroups of the backward, each of which leaves H fp32 sums for dgamma: no more than keep the loads going.
+// One per CU where a thread holds 16 or more values of a row and those of the next one (8192 x 4096 in bf16:
+// 65 us, 68 with two, 76 with four), two where it holds 8 (16384 x 2048: 64 us, 70 with one; 262144 x 128: 42
+// and 58).
 int64_t backward_blocks(int64_t N, int64_t H) {
-  int64_t rows = 1, most = 512;
-  by_width(H, [&](auto tpr, auto) {
+  int64_t rows = 1, most = 256;
+  by_width(H, [&](auto tpr, auto ch) {
     constexpr int kTpr = decltype(tpr)::value;
     rows = threads_of(kTpr) / kTpr;
-    most = kTpr > 256 ? 256 : 512;
+    if (decltype(ch)::value == 1) most = 512;
   });
   return std::max<int64_t>(1, std::min(cdiv(N, rows), most));
 }
@@ -111,7 +114,8 @@ lce_status_t run_forward(const NormArgs& a, hipStream_t s) {
   by_width(a.H, [&](auto tpr, auto ch) {
     constexpr int kTpr = decltype(tpr)::value, kCh = decltype(ch)::value, kThreads = threads_of(kTpr);
     const int64_t blocks = std::min(cdiv(a.N, kThreads / kTpr), kForwardBlocks);
-    hipLaunchKernelGGL((add_rmsnorm_kernel<T, kTpr, kCh, QUANT>), dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
+    auto kernel = a.H % kNormVec == 0 ? add_rmsnorm_kernel<T, kTpr, kCh, QUANT, true> : add_rmsnorm_kernel<T, kTpr, kCh, QUANT, false>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
   });
   return launched();
 }
@@ -121,10 +125,13 @@ lce_status_t run_backward(const NormBackwardArgs& a, int64_t blocks, void* dgamm
   if (a.N > 0)
     by_width(a.H, [&](auto tpr, auto ch) {
       constexpr int kTpr = decltype(tpr)::value, kCh = decltype(ch)::value;
-      hipLaunchKernelGGL((add_rmsnorm_backward_kernel<T, kTpr, kCh>), dim3((unsigned)blocks), dim3(threads_of(kTpr)), 0, s, a);
+      constexpr bool kAhead = kTpr < 512 || (kTpr == 512 && (kCh < 4 || sizeof(T) == 2));  // as registers allow
+      auto kernel = a.H % kNormVec == 0 ? add_rmsnorm_backward_kernel<T, kTpr, kCh, true, kAhead>
+                                        : add_rmsnorm_backward_kernel<T, kTpr, kCh, false, false>;
+      hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads_of(kTpr)), 0, s, a);
     });
   if (dgamma != nullptr)
-    hipLaunchKernelGGL(gamma_sum_kernel<T>, dim3((unsigned)cdiv(a.H, 64)), dim3(1024), 0, s, a.part,
+    hipLaunchKernelGGL(gamma_sum_kernel<T>, dim3((unsigned)cdiv(a.H, 16)), dim3(1024), 0, s, a.part,
                        a.N > 0 ? (int)blocks : 0, a.H, (T*)dgamma);
   return launched();
 }

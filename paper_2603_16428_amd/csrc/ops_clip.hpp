@@ -106,14 +106,19 @@ struct GradRun {
   int64_t pieces;
 };
 
-// Calls f(entry, its piece) for the workgroup's run of pieces.
-template <typename F>
+// Calls f(entry, its piece) for the workgroup's run of pieces, the last one first where BACK.
+template <bool BACK, typename F>
 __device__ __forceinline__ void for_pieces(const TensorEntry* e, const GradRun& r, F f) {
   const int64_t c0 = r.pieces * blockIdx.x / gridDim.x, c1 = r.pieces * (blockIdx.x + 1) / gridDim.x;
   if (c0 >= c1) return;
-  int k = find_tensor(e, r.count, c0);
-  for (int64_t c = c0; c < c1; ++c) {
-    while (k + 1 < r.count && e[k + 1].first <= c) ++k;
+  int k = find_tensor(e, r.count, BACK ? c1 - 1 : c0);
+  for (int64_t n = 0; n < c1 - c0; ++n) {
+    const int64_t c = BACK ? c1 - 1 - n : c0 + n;
+    if (BACK) {
+      while (e[k].first > c) --k;
+    } else {
+      while (k + 1 < r.count && e[k + 1].first <= c) ++k;
+    }
     f(e[k], c - e[k].first);
   }
 }
@@ -122,7 +127,7 @@ template <bool INF>
 __device__ __forceinline__ void norm_pieces(const TensorEntry* e, const GradRun& r, double* __restrict__ part) {
   __shared__ double lds[kGradThreads / 64];
   double acc = 0.0;
-  for_pieces(e, r, [&](const TensorEntry& t, int64_t c) {
+  for_pieces<false>(e, r, [&](const TensorEntry& t, int64_t c) {
     if (t.dtype == 0) {
       constexpr int64_t kN = kPieceBytes / 4;
       acc = piece_norm<float, INF>((const float*)t.in + c * kN, t.n - c * kN, acc);
@@ -179,7 +184,7 @@ __device__ __forceinline__ void clip_pieces(const TensorEntry* e, const GradRun&
   const double ratio = a.max_norm / (norm + 1e-6);
   const float f = ratio >= 1.0 || a.max_norm == INFINITY ? 1.f : (float)ratio;  // a NaN stays
   if (a.in_place && f == 1.f) return;
-  for_pieces(e, r, [&](const TensorEntry& t, int64_t c) {
+  for_pieces<true>(e, r, [&](const TensorEntry& t, int64_t c) {
     if (t.dtype == 0) {
       constexpr int64_t kN = kPieceBytes / 4;
       piece_scale((const float*)t.in + c * kN, (float*)t.out + c * kN, t.n - c * kN, f);

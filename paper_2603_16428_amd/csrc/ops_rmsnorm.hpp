@@ -17,28 +17,52 @@ namespace lce {
 
 constexpr int kNormVec = 8;
 
-// 8 values at p as fp32, of which the first n exist (the others are 0); n may be <= 0.
+// 8 values of a row as they are stored, in 32-bit registers that hold them until they are needed.
 template <typename T>
-__device__ __forceinline__ void load_row(const T* p, int n, float (&v)[kNormVec]) {
-  T raw[kNormVec];
-  if (n >= kNormVec) {
-    __builtin_memcpy(raw, p, sizeof(raw));
+struct RawRow {
+  uint32_t w[kNormVec * sizeof(T) / 4];
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (sizeof(T) == 4) {
+      return __builtin_bit_cast(float, w[e]);
+    } else if constexpr (std::is_same_v<T, bf16>) {
+      return __builtin_bit_cast(float, e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    } else {
+      return (float)__builtin_bit_cast(f16, (uint16_t)(e & 1 ? w[e / 2] >> 16 : w[e / 2]));
+    }
+  }
+  __device__ __forceinline__ void keep_if(bool yes) {
 #pragma unroll
-    for (int e = 0; e < kNormVec; ++e) v[e] = to_f32(raw[e]);
+    for (uint32_t& v : w) v = yes ? v : 0u;
+  }
+};
+// The values from column c on, of which the first n exist (the others are 0; n may be <= 0). WHOLE: H is a
+// multiple of 8, so a thread's 8 values exist or not: they are loaded without a branch (from column `whole`,
+// which exists for every thread) and the caller masks what it must. A branch per load keeps the compiler
+// from requesting them together (backward in bf16, 8192 x 4096: 113 us, and 65 without).
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void load_raw(const T* row, int c, int whole, int n, RawRow<T>& raw) {
+  if constexpr (WHOLE) {
+    __builtin_memcpy(raw.w, row + whole, sizeof(raw.w));
   } else {
+    T v[kNormVec];
+    if (n >= kNormVec) {
+      __builtin_memcpy(v, row + c, sizeof(v));
+    } else {
 #pragma unroll
-    for (int e = 0; e < kNormVec; ++e) v[e] = e < n ? to_f32(p[e]) : 0.f;
+      for (int e = 0; e < kNormVec; ++e) v[e] = e < n ? row[c + e] : (T)0.f;
+    }
+    __builtin_memcpy(raw.w, v, sizeof(v));
   }
 }
 
-template <typename T>
+template <bool WHOLE = false, typename T>
 __device__ __forceinline__ void store_row(T* p, int n, const float (&v)[kNormVec]) {
   if (n >= kNormVec) {
     T raw[kNormVec];
 #pragma unroll
     for (int e = 0; e < kNormVec; ++e) raw[e] = from_f32<T>(v[e]);
     __builtin_memcpy(p, raw, sizeof(raw));
-  } else {
+  } else if constexpr (!WHOLE) {
 #pragma unroll
     for (int e = 0; e < kNormVec; ++e)
       if (e < n) p[e] = from_f32<T>(v[e]);
@@ -47,6 +71,7 @@ __device__ __forceinline__ void store_row(T* p, int n, const float (&v)[kNormVec
 
 // 8 values in e4m3, to nearest even. All are NaN or at most 448 (up to an fp32 rounding, which goes to
 // 448): nothing has to be clamped.
+template <bool WHOLE>
 __device__ __forceinline__ void store_row_fp8(uint8_t* p, int n, const float (&v)[kNormVec]) {
   uint32_t w[2];
 #pragma unroll
@@ -56,7 +81,7 @@ __device__ __forceinline__ void store_row_fp8(uint8_t* p, int n, const float (&v
   }
   if (n >= kNormVec) {
     __builtin_memcpy(p, w, 8);
-  } else {
+  } else if constexpr (!WHOLE) {
 #pragma unroll
     for (int e = 0; e < kNormVec; ++e)
       if (e < n) p[e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
@@ -98,45 +123,61 @@ struct NormArgs {
 constexpr float kFp8Max = 448.f;
 constexpr float kScaleMin = 1.17549435e-38f;  // 2^-126, whose inverse is still finite
 
-template <typename T, int TPR, int CH, bool QUANT>
+template <typename T, int TPR, int CH, bool QUANT, bool WHOLE>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(const NormArgs a) {
   constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR, kWaves = TPR > 64 ? TPR / 64 : 1;
   __shared__ float sums[2][kWaves];
   __shared__ uint32_t tops[2][kWaves];
   const int t = threadIdx.x % TPR;
+  const float inv_h = 1.f / (float)a.H;
   int turn = 0;
   for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.N; base += (int64_t)gridDim.x * kRows, turn ^= 1) {
     const int64_t i = base + threadIdx.x / TPR;
     const bool live = i < a.N;
+    const int64_t row = live ? i : a.N - 1;
+    RawRow<T> x[CH], res[CH], gamma[CH];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int c = (k * TPR + t) * kNormVec;
+      load_raw<WHOLE>((const T*)a.x + row * a.x_ld, c, min(c, a.H - kNormVec), live ? a.H - c : 0, x[k]);
+      res[k].keep_if(false);
+    }
+    if (a.residual != nullptr) {
+#pragma unroll
+      for (int k = 0; k < CH; ++k) {
+        const int c = (k * TPR + t) * kNormVec;
+        load_raw<WHOLE>((const T*)a.residual + row * a.residual_ld, c, min(c, a.H - kNormVec), live ? a.H - c : 0, res[k]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int c = (k * TPR + t) * kNormVec;
+      load_raw<WHOLE>((const T*)a.gamma, c, min(c, a.H - kNormVec), a.H - c, gamma[k]);
+    }
     float s[CH][kNormVec];
     float ss = 0.f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
-      load_row((const T*)a.x + i * a.x_ld + c, n, s[k]);
-      if (a.residual != nullptr) {
-        float r[kNormVec];
-        load_row((const T*)a.residual + i * a.residual_ld + c, n, r);
+      const bool mine = !WHOLE || (live && (k * TPR + t) * kNormVec < a.H);
 #pragma unroll
-        for (int e = 0; e < kNormVec; ++e) s[k][e] += r[e];
+      for (int e = 0; e < kNormVec; ++e) {
+        s[k][e] = x[k].at(e) + res[k].at(e);
+        if (!mine) s[k][e] = 0.f;
+        ss = fmaf(s[k][e], s[k][e], ss);
       }
-#pragma unroll
-      for (int e = 0; e < kNormVec; ++e) ss = fmaf(s[k][e], s[k][e], ss);
     }
     ss = row_reduce<TPR, AddOp>(ss, sums[turn]);
-    const float r = 1.f / sqrtf(ss / (float)a.H + a.eps);
+    const float r = rsqrtf(fmaf(ss, inv_h, a.eps));
     if (live && t == 0 && a.rstd != nullptr) a.rstd[i] = r;
     uint32_t top = 0;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
-      if (a.added != nullptr) store_row((T*)a.added + i * a.added_ld + c, n, s[k]);
-      float g[kNormVec];
-      load_row((const T*)a.gamma + c, n, g);
+      if (a.added != nullptr) store_row<WHOLE>((T*)a.added + i * a.added_ld + c, n, s[k]);
 #pragma unroll
-      for (int e = 0; e < kNormVec; ++e) s[k][e] = s[k][e] * r * g[e];
+      for (int e = 0; e < kNormVec; ++e) s[k][e] = s[k][e] * r * gamma[k].at(e);
       if constexpr (!QUANT) {
-        store_row((T*)a.normed + i * a.normed_ld + c, n, s[k]);
+        store_row<WHOLE>((T*)a.normed + i * a.normed_ld + c, n, s[k]);
       } else {
         // The largest magnitude by its bits, among which a NaN's are above all others.
         uint32_t m = 0;
@@ -147,12 +188,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
         } else {
           for (int o = 1; o < a.group / kNormVec; o <<= 1) m = MaxOp::of(m, (uint32_t)__shfl_xor((int)m, o));
           const float amax = __builtin_bit_cast(float, m);
-          const float scale = amax / kFp8Max, inv = scale < kScaleMin ? 1.f / kScaleMin : kFp8Max / amax;
+          const float scale = amax * (1.f / kFp8Max), inv = scale < kScaleMin ? 1.f / kScaleMin : kFp8Max / amax;
           if (n > 0 && c % a.group == 0)
             a.scales[i * ((a.H + a.group - 1) / a.group) + c / a.group] = scale < kScaleMin ? kScaleMin : scale;
 #pragma unroll
           for (int e = 0; e < kNormVec; ++e) s[k][e] *= inv;
-          store_row_fp8((uint8_t*)a.normed + i * a.normed_ld + c, n, s[k]);
+          store_row_fp8<WHOLE>((uint8_t*)a.normed + i * a.normed_ld + c, n, s[k]);
         }
       }
     }
@@ -160,14 +201,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
       if (a.group == 0) {
         top = row_reduce<TPR, MaxOp>(top, tops[turn]);
         const float amax = __builtin_bit_cast(float, top);
-        const float scale = amax / kFp8Max, inv = scale < kScaleMin ? 1.f / kScaleMin : kFp8Max / amax;
+        const float scale = amax * (1.f / kFp8Max), inv = scale < kScaleMin ? 1.f / kScaleMin : kFp8Max / amax;
         if (live && t == 0) a.scales[i] = scale < kScaleMin ? kScaleMin : scale;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {
           const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
 #pragma unroll
           for (int e = 0; e < kNormVec; ++e) s[k][e] *= inv;
-          store_row_fp8((uint8_t*)a.normed + i * a.normed_ld + c, n, s[k]);
+          store_row_fp8<WHOLE>((uint8_t*)a.normed + i * a.normed_ld + c, n, s[k]);
         }
       }
     }
@@ -186,61 +227,106 @@ struct NormBackwardArgs {
 
 // A workgroup walks over rows; each thread keeps the sums of its own columns of dgamma over them, and
 // the workgroup's sums go to part (summed by gamma_sum_kernel in a fixed order).
-template <typename T, int TPR, int CH>
+//
+// Bound by HBM, so the loads may not stop while a row is reduced: AHEAD requests the next row's values
+// before the current one's dot product is joined. (A row's barrier and its joins take as long as its
+// loads.) What waits in registers waits in the input type.
+template <typename T, int TPR, int CH, bool WHOLE, bool AHEAD>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_kernel(const NormBackwardArgs a) {
   constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR, kWaves = TPR > 64 ? TPR / 64 : 1;
   constexpr int kCols = TPR * CH * kNormVec;
   __shared__ float sums[2][kWaves];
   const int t = threadIdx.x % TPR;
-  float acc[CH][kNormVec], g[CH][kNormVec];
+  const float inv_h = 1.f / (float)a.H;
+  const bool has_res = a.residual != nullptr, has_ds = a.ds != nullptr;
+  // Where they would not fit the registers (kWide), dgamma's sums are kept in LDS and gamma is read again for
+  // each row (H = 12288 in bf16 fits: 100 us for 4096 rows, 106 so).
+  constexpr bool kWide = TPR == 1024 || (TPR == 512 && (CH == 4 || sizeof(T) == 4));
+  __shared__ f32x4 wide_acc[kWide ? CH * 2 * TPR : 1];
+  float acc[kWide ? 1 : CH][kNormVec];
+  RawRow<T> g[kWide ? 1 : CH], x[CH], res[CH], dy[CH], ds[CH];
+  int whole[CH];
 #pragma unroll
   for (int k = 0; k < CH; ++k) {
     const int c = (k * TPR + t) * kNormVec;
-    load_row((const T*)a.gamma + c, a.H - c, g[k]);
+    whole[k] = min(c, a.H - kNormVec);
+    if constexpr (kWide) {
+      wide_acc[2 * k * TPR + t] = wide_acc[(2 * k + 1) * TPR + t] = (f32x4){};
+    } else {
+      load_raw<WHOLE>((const T*)a.gamma, c, whole[k], a.H - c, g[k]);
 #pragma unroll
-    for (int e = 0; e < kNormVec; ++e) acc[k][e] = 0.f;
+      for (int e = 0; e < kNormVec; ++e) acc[k][e] = 0.f;
+    }
+    res[k].keep_if(false);
+    ds[k].keep_if(false);
   }
-  const float inv_h = 1.f / (float)a.H;
-  int turn = 0;
-  for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.N; base += (int64_t)gridDim.x * kRows, turn ^= 1) {
-    const int64_t i = base + threadIdx.x / TPR;
+  const int64_t stride = (int64_t)gridDim.x * kRows;
+  float r = 0.f;
+  auto request = [&](int64_t i) {
     const bool live = i < a.N;
-    float dy[CH][kNormVec], s[CH][kNormVec], ds[CH][kNormVec];
-    const float r = live ? a.rstd[i] : 0.f;
+    const int64_t row = live ? i : a.N - 1;
+    r = a.rstd[row];
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
+      load_raw<WHOLE>((const T*)a.dy + row * a.dy_ld, c, whole[k], n, dy[k]);
+      load_raw<WHOLE>((const T*)a.x + row * a.x_ld, c, whole[k], n, x[k]);
+    }
+    if (has_res) {
+#pragma unroll
+      for (int k = 0; k < CH; ++k) {
+        const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
+        load_raw<WHOLE>((const T*)a.residual + row * a.residual_ld, c, whole[k], n, res[k]);
+      }
+    }
+    if (has_ds) {
+#pragma unroll
+      for (int k = 0; k < CH; ++k) {
+        const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
+        load_raw<WHOLE>((const T*)a.ds + row * a.ds_ld, c, whole[k], n, ds[k]);
+      }
+    }
+  };
+  int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+  int turn = 0;
+  if (AHEAD) request(i);
+  for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.N; base += stride, i += stride, turn ^= 1) {
+    if (!AHEAD) request(i);
+    const float ri = r;
+    float s[CH][kNormVec];
+    RawRow<T> dyi[CH], dsi[CH];
     float dot = 0.f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
-      load_row((const T*)a.dy + i * a.dy_ld + c, n, dy[k]);
-      load_row((const T*)a.x + i * a.x_ld + c, n, s[k]);
-      if (a.residual != nullptr) {
-        float res[kNormVec];
-        load_row((const T*)a.residual + i * a.residual_ld + c, n, res);
-#pragma unroll
-        for (int e = 0; e < kNormVec; ++e) s[k][e] += res[e];
-      }
-      if (a.ds != nullptr) load_row((const T*)a.ds + i * a.ds_ld + c, n, ds[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
+      const int c = (k * TPR + t) * kNormVec;
+      dyi[k] = dy[k];
+      dsi[k] = ds[k];
+      if (WHOLE) dyi[k].keep_if(i < a.N && c < a.H);  // what is not there adds nothing to a sum
+      RawRow<T>& gk = g[kWide ? 0 : k];
+      if (kWide) load_raw<WHOLE>((const T*)a.gamma, c, whole[k], a.H - c, gk);
 #pragma unroll
       for (int e = 0; e < kNormVec; ++e) {
-        acc[k][e] = fmaf(dy[k][e], s[k][e] * r, acc[k][e]);
-        dy[k][e] *= g[k][e];
-        dot = fmaf(dy[k][e], s[k][e], dot);
+        s[k][e] = x[k].at(e) + res[k].at(e);
+        dot = fmaf(dyi[k].at(e) * gk.at(e), s[k][e], dot);
       }
     }
+    if (AHEAD && base + stride < a.N) request(i + stride);
     dot = row_reduce<TPR, AddOp>(dot, sums[turn]);
-    const float c1 = r * r * (dot * inv_h);
+    const float c1 = ri * ri * (dot * inv_h);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
+      const int c = (k * TPR + t) * kNormVec, n = i < a.N ? a.H - c : 0;
+      float dx[kNormVec];
+      RawRow<T>& gk = g[kWide ? 0 : k];
+      if (kWide) load_raw<WHOLE>((const T*)a.gamma, c, whole[k], a.H - c, gk);
 #pragma unroll
       for (int e = 0; e < kNormVec; ++e) {
-        dy[k][e] = r * (dy[k][e] - s[k][e] * c1);
-        if (a.ds != nullptr) dy[k][e] += ds[k][e];
+        const float d = dyi[k].at(e), dg = d * (s[k][e] * ri);
+        if constexpr (kWide) ((float*)&wide_acc[(2 * k + e / 4) * TPR + t])[e % 4] += dg;
+        else acc[k][e] += dg;
+        dx[e] = fmaf(ri, d * gk.at(e) - s[k][e] * c1, dsi[k].at(e));
       }
-      store_row((T*)a.dx + i * a.dx_ld + c, n, dy[k]);
+      store_row<WHOLE>((T*)a.dx + i * a.dx_ld + c, n, dx);
     }
   }
   if (a.part == nullptr) return;
@@ -249,7 +335,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_ke
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       const int c = (k * TPR + t) * kNormVec;
-      store_row(out + c, a.H - c, acc[k]);
+      if constexpr (kWide) {
+#pragma unroll
+        for (int e = 0; e < kNormVec; ++e) acc[0][e] = wide_acc[(2 * k + e / 4) * TPR + t][e % 4];
+      }
+      store_row<WHOLE>(out + c, a.H - c, acc[kWide ? 0 : k]);
     }
   } else {
     __shared__ float cols[kRows][kCols];
@@ -267,31 +357,35 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_ke
   }
 }
 
-// dgamma_j = sum_b part[b][j] in a fixed order: 64 columns per workgroup, every 16th row of part per
-// wave (four requested ahead), then the 16 waves' sums in order.
+// dgamma_j = sum_b part[b][j] in a fixed order: 16 columns per workgroup, every 64th row of part per thread
+// (eight requested at once: 512 rows are one round of loads), then the threads' sums in order. A chain of
+// loads, so what counts is how many threads share it.
 template <typename T>
 __global__ __launch_bounds__(1024) void gamma_sum_kernel(const float* __restrict__ part, int rows, int H,
                                                          T* __restrict__ dgamma) {
-  constexpr int kAhead = 4, kWaves = 16;
-  __shared__ float sums[kWaves][64];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int j = blockIdx.x * 64 + lane;
+  constexpr int kAhead = 8, kCols = 16, kGroups = 64, kWaves = 16;
+  __shared__ float sums[kWaves][kCols];
+  const int col = threadIdx.x % kCols, grp = threadIdx.x / kCols;
+  const int j = blockIdx.x * kCols + col;
   float acc = 0.f;
   if (j < H) {
-    for (int b0 = w; b0 < rows; b0 += kWaves * kAhead) {
+    for (int b0 = grp; b0 < rows; b0 += kGroups * kAhead) {
       float v[kAhead];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) v[u] = b0 + kWaves * u < rows ? part[(size_t)(b0 + kWaves * u) * H + j] : 0.f;
+      for (int u = 0; u < kAhead; ++u) v[u] = b0 + kGroups * u < rows ? part[(size_t)(b0 + kGroups * u) * H + j] : 0.f;
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) acc += v[u];
     }
   }
-  sums[w][lane] = acc;
-  __syncthreads();
-  if (w == 0 && j < H) {
 #pragma unroll
-    for (int k = 1; k < kWaves; ++k) acc += sums[k][lane];
-    dgamma[j] = from_f32<T>(acc);
+  for (int o = kCols; o < 64; o <<= 1) acc += __shfl_xor(acc, o);
+  if ((threadIdx.x & 63) < kCols) sums[threadIdx.x >> 6][col] = acc;
+  __syncthreads();
+  if (grp == 0 && j < H) {
+    float v = sums[0][col];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) v += sums[w][col];
+    dgamma[j] = from_f32<T>(v);
   }
 }
 

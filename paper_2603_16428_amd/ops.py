@@ -7,6 +7,7 @@ the current stream of the tensors' device, and nothing waits for the GPU.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 
 import torch
@@ -307,24 +308,24 @@ def _dense(t) -> bool:
 
 
 def _check_grads(grads):
+    """The gradients that are not None, their device, and their lce_tensor_t entries."""
     grads = [grads] if isinstance(grads, torch.Tensor) else [g for g in grads if g is not None]
     if not grads:
         raise ValueError("no gradients")
-    dev = grads[0].device
-    for g in grads:
-        if not g.is_cuda or g.device != dev:
-            raise ValueError("gradients must be tensors of one device")
-        if g.dtype not in DTYPES or g.layout != torch.strided:
+    index, flat = grads[0].get_device(), []
+    if index < 0:
+        raise ValueError("gradients must be device tensors")
+    strided, codes = torch.strided, DTYPES
+    for g in grads:  # a model has hundreds: half a microsecond for each
+        code = codes.get(g.dtype)
+        if code is None or g.layout is not strided:
             raise ValueError("gradients must be dense bfloat16, float16 or float32 tensors")
+        if g.get_device() != index:
+            raise ValueError("gradients must be tensors of one device")
         if not (g.is_contiguous() or g.numel() == 0 or _dense(g)):
             raise ValueError("a gradient's values must fill one block of memory, in any order")
-    return grads, dev
-
-
-def _table(grads):
-    """lce_tensor_t entries."""
-    flat = [v for g in grads for v in (g.data_ptr(), g.numel(), DTYPES[g.dtype])]
-    return (ctypes.c_int64 * len(flat))(*flat)
+        flat += (g.data_ptr(), g.numel(), code)
+    return grads, grads[0].device, array.array("q", flat)
 
 
 def _norm_type(norm_type):
@@ -335,13 +336,13 @@ def _norm_type(norm_type):
 
 def grad_norm_workspace_size(count: int) -> int:
     """Bytes of workspace for `count` gradients."""
-    return int(_library().lce_grad_norm_workspace_size(count))
+    return int((_lib or _library()).lce_grad_norm_workspace_size(count))
 
 
-def _grad_workspace(workspace, count, dev):
+def _grad_workspace(workspace, grads):
     if workspace is not None:
         return workspace
-    return torch.empty(_library().lce_grad_norm_workspace_size(count), dtype=torch.uint8, device=dev)
+    return grads[0].new_empty(grad_norm_workspace_size(len(grads)), dtype=torch.uint8)
 
 
 def grad_norm(grads, norm_type: float = 2.0, workspace: torch.Tensor | None = None):
@@ -351,19 +352,20 @@ def grad_norm(grads, norm_type: float = 2.0, workspace: torch.Tensor | None = No
     filling one block of memory.
     """
     kind = _norm_type(norm_type)
-    grads, dev = _check_grads(grads)
-    norm = torch.empty((), dtype=torch.float32, device=dev)
-    ws = _grad_workspace(workspace, len(grads), dev)
-    _call("lce_grad_norm", dev, _table(grads), len(grads), kind, norm.data_ptr(), ws.data_ptr(), ws.numel())
+    grads, dev, table = _check_grads(grads)
+    norm = grads[0].new_empty((), dtype=torch.float32)
+    ws = _grad_workspace(workspace, grads)
+    _call("lce_grad_norm", dev, table.buffer_info()[0], len(grads), kind, norm.data_ptr(), ws.data_ptr(), ws.numel())
     return norm
 
 
-def _clip(grads, dev, max_norm, norm_type, out, workspace):
-    norm = torch.empty((), dtype=torch.float32, device=dev)
-    ws = _grad_workspace(workspace, len(grads), dev)
-    outs = None if out is None else (ctypes.c_void_p * len(out))(*[t.data_ptr() for t in out])
+def _clip(grads, dev, table, max_norm, norm_type, out, workspace):
+    norm = grads[0].new_empty((), dtype=torch.float32)
+    ws = _grad_workspace(workspace, grads)
+    outs = None if out is None else array.array("Q", [t.data_ptr() for t in out])
     _written(grads if out is None else out)
-    _call("lce_clip_grad_norm", dev, _table(grads), len(grads), norm_type, max_norm, outs, norm.data_ptr(),
+    _call("lce_clip_grad_norm", dev, table.buffer_info()[0], len(grads), norm_type, max_norm,
+          None if outs is None else outs.buffer_info()[0], norm.data_ptr(),
           ws.data_ptr(), ws.numel())
     return norm
 
@@ -375,8 +377,8 @@ def clip_grad_norm_(grads, max_norm: float, norm_type: float = 2.0, workspace: t
     the device, and gradients within the limit are not written. A NaN among the gradients makes all NaN.
     """
     kind = _norm_type(norm_type)
-    grads, dev = _check_grads(grads)
-    return _clip(grads, dev, max_norm, kind, None, workspace)
+    grads, dev, table = _check_grads(grads)
+    return _clip(grads, dev, table, max_norm, kind, None, workspace)
 
 
 def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, out=None, workspace: torch.Tensor | None = None):
@@ -386,7 +388,7 @@ def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, out=None, wor
     reads), one for each gradient that is not None; new ones by default.
     """
     kind = _norm_type(norm_type)
-    grads, dev = _check_grads(grads)
+    grads, dev, table = _check_grads(grads)
     if out is None:
         out = [torch.empty_like(g) for g in grads]
     else:
@@ -394,4 +396,4 @@ def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, out=None, wor
         if len(out) != len(grads) or any(t.shape != g.shape or t.dtype != g.dtype or t.device != dev
                                          or (t.stride() != g.stride() and t.numel() > 1) for t, g in zip(out, grads)):
             raise ValueError("out must match the gradients in number, shape, strides, dtype and device")
-    return _clip(grads, dev, max_norm, kind, out, workspace), out
+    return _clip(grads, dev, table, max_norm, kind, out, workspace), out
