@@ -242,6 +242,7 @@ lce_status_t grad_norm_call(const lce_tensor_t* grads, int64_t count, int norm_t
     if (pieces < 0) return LCE_ERR_UNSUPPORTED;
     if (clip && clip_overlaps(table)) return LCE_ERR_INVALID_ARGUMENT;
     if (!workspace || workspace_bytes < lce_grad_norm_workspace_size(count)) return LCE_ERR_WORKSPACE_TOO_SMALL;
+    if ((uintptr_t)workspace % 256 != 0) return LCE_ERR_INVALID_ARGUMENT;
     return norm_type == LCE_NORM_INF ? run_norm<true>(table, pieces, clip, out == nullptr, max_norm, norm, workspace, s)
                                      : run_norm<false>(table, pieces, clip, out == nullptr, max_norm, norm, workspace, s);
   } catch (...) {
@@ -338,8 +339,10 @@ lce_status_t lce_add_rmsnorm_backward(const void* grad_normed, int64_t grad_norm
                              {{gamma, H * z, H * z, 1}, {rstd, 4, 4, N}});
     if (st != LCE_OK) return st;
   }
-  if (grad_gamma != nullptr && (!workspace || workspace_bytes < lce_add_rmsnorm_workspace_size(N, H, dtype)))
-    return LCE_ERR_WORKSPACE_TOO_SMALL;
+  if (grad_gamma != nullptr) {
+    if (!workspace || workspace_bytes < lce_add_rmsnorm_workspace_size(N, H, dtype)) return LCE_ERR_WORKSPACE_TOO_SMALL;
+    if ((uintptr_t)workspace % 256 != 0) return LCE_ERR_INVALID_ARGUMENT;
+  }
   if (N == 0 && grad_gamma == nullptr) return LCE_OK;
   const lce::NormBackwardArgs a{grad_normed, grad_added, x, residual, gamma, rstd, grad_hidden,
                                 grad_gamma != nullptr ? (float*)workspace : nullptr, grad_normed_ld, grad_added_ld,

@@ -161,8 +161,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
       const bool mine = !WHOLE || (live && (k * TPR + t) * kNormVec < a.H);
 #pragma unroll
       for (int e = 0; e < kNormVec; ++e) {
-        s[k][e] = x[k].at(e) + res[k].at(e);
-        if (!mine) s[k][e] = 0.f;
+        s[k][e] = mine ? x[k].at(e) + res[k].at(e) : 0.f;
         ss = fmaf(s[k][e], s[k][e], ss);
       }
     }
@@ -301,12 +300,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_ke
       const int c = (k * TPR + t) * kNormVec;
       dyi[k] = dy[k];
       dsi[k] = ds[k];
-      if (WHOLE) dyi[k].keep_if(i < a.N && c < a.H);  // what is not there adds nothing to a sum
+      // What is not there adds nothing to a sum (nor does what another row in place is just writing there).
+      const bool mine = !WHOLE || (i < a.N && c < a.H);
+      dyi[k].keep_if(mine);
       RawRow<T>& gk = g[kWide ? 0 : k];
       if (kWide) load_raw<WHOLE>((const T*)a.gamma, c, whole[k], a.H - c, gk);
 #pragma unroll
       for (int e = 0; e < kNormVec; ++e) {
-        s[k][e] = x[k].at(e) + res[k].at(e);
+        s[k][e] = mine ? x[k].at(e) + res[k].at(e) : 0.f;
         dot = fmaf(dyi[k].at(e) * gk.at(e), s[k][e], dot);
       }
     }

@@ -50,6 +50,15 @@ _device_index = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+def _space(workspace, like, nbytes: int):
+    """A given workspace (its size is the library's to check), or a new one."""
+    if workspace is None:
+        return like.new_empty(nbytes, dtype=torch.uint8)
+    if workspace.dtype is not torch.uint8 or workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 tensor on the tensors' device")
+    return workspace
+
+
 def _call(name: str, device, *args) -> None:
     """A library call on the current stream of `device`, with that device the current one."""
     f = getattr(_lib or _library(), name)
@@ -92,7 +101,7 @@ def _optional(t, what: str):
 
 
 def _check_rows(hidden, gamma):
-    """(N, H, device, shape) of rows and their gain."""
+    """(N, H, shape, dtype, device) of rows and their gain."""
     if not hidden.is_cuda:
         raise ValueError("hidden must be a device tensor")
     shape, dtype, dev = hidden.shape, hidden.dtype, hidden.device
@@ -105,11 +114,11 @@ def _check_rows(hidden, gamma):
         raise ValueError("gamma must be [H] of the hidden dtype, on the hidden's device")
     if not gamma.is_contiguous() or gamma.is_neg() or hidden.is_neg():
         raise ValueError("gamma must be contiguous, and nothing a lazily negated view")
-    return hidden.numel() // H, H, dev, shape
+    return hidden.numel() // H, H, shape, dtype, dev
 
 
-def _check_like(t, hidden, what: str):
-    if t.shape != hidden.shape or t.dtype != hidden.dtype or t.device != hidden.device:
+def _check_like(t, shape, dtype, dev, what: str):
+    if t.shape != shape or t.dtype is not dtype or t.device != dev:
         raise ValueError(f"{what} must have the hidden's shape, dtype and device")
     if t.is_neg():
         raise ValueError(f"{what} is a lazily negated view: resolve_neg() it first")
@@ -123,19 +132,18 @@ def _written(tensors) -> None:
         torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
 
 
-def _output(t, like, what: str, dtype=None):
-    """A given output, checked, or a new one."""
+def _output(t, like, dtype, what: str):
+    """A given output, checked, or a new one: rows of `like`'s shape."""
     if t is None:
-        return like.new_empty(like.shape, dtype=dtype)
-    if t.shape != like.shape or t.dtype != (dtype or like.dtype) or t.device != like.device:
-        raise ValueError(f"{what} must have the hidden's shape and device and dtype {dtype or like.dtype}")
+        return torch.empty_like(like, dtype=dtype) if like.is_contiguous() else like.new_empty(like.shape, dtype=dtype)
+    _check_like(t, like.shape, dtype, like.device, what)
     _written([t])
     return t
 
 
 def _run_forward(hidden, residual, gamma, eps, quant, group_size, normed, added, return_rstd):
-    N, H, dev, shape = _check_rows(hidden, gamma)
-    out = _output(normed, hidden, "normed", FP8 if quant else None)
+    N, H, shape, dtype, dev = _check_rows(hidden, gamma)
+    out = _output(normed, hidden, FP8 if quant else dtype, "normed")
     scales = None
     if quant:
         scales = hidden.new_empty(shape[:-1] + (-(-H // group_size) if group_size else 1,), dtype=torch.float32)
@@ -144,12 +152,12 @@ def _run_forward(hidden, residual, gamma, eps, quant, group_size, normed, added,
             raise ValueError("without a residual there is no sum: it is hidden itself")
         total = hidden
     else:
-        _check_like(residual, hidden, "residual")
-        total = _output(added, hidden, "added")
+        _check_like(residual, shape, dtype, dev, "residual")
+        total = _output(added, hidden, dtype, "added")
     rstd = hidden.new_empty(shape[:-1], dtype=torch.float32) if return_rstd else None
     if N:
         rows = (hidden.data_ptr(), _pitch(hidden, "hidden"), *_optional(residual, "residual"), gamma.data_ptr(), N, H,
-                DTYPES[hidden.dtype], eps)
+                DTYPES[dtype], eps)
         sums = _optional(None if residual is None else total, "added")
         r = None if rstd is None else rstd.data_ptr()
         if quant:
@@ -200,26 +208,26 @@ def add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd,
     and of the residual alike; it may be given, and may be grad_normed, grad_added, hidden or residual
     themselves. grad_gamma is None without need_gamma.
     """
-    N, H, dev, shape = _check_rows(hidden, gamma)
-    _check_like(grad_normed, hidden, "grad_normed")
+    N, H, shape, dtype, dev = _check_rows(hidden, gamma)
+    _check_like(grad_normed, shape, dtype, dev, "grad_normed")
     if grad_added is not None:
-        _check_like(grad_added, hidden, "grad_added")
+        _check_like(grad_added, shape, dtype, dev, "grad_added")
     if residual is not None:
-        _check_like(residual, hidden, "residual")
+        _check_like(residual, shape, dtype, dev, "residual")
     if rstd.shape != shape[:-1] or rstd.dtype != torch.float32 or rstd.device != dev or not rstd.is_contiguous():
         raise ValueError("rstd must be the forward call's")
-    dx = _output(grad_hidden, hidden, "grad_hidden")
+    dx = _output(grad_hidden, hidden, dtype, "grad_hidden")
     dg = torch.empty_like(gamma) if need_gamma else None
     if N or need_gamma:
         ws = None
         if need_gamma:
-            need = (_lib or _library()).lce_add_rmsnorm_workspace_size(N, H, DTYPES[hidden.dtype])
+            need = (_lib or _library()).lce_add_rmsnorm_workspace_size(N, H, DTYPES[dtype])
             if need == 0:
                 raise LCEError(2, "lce_add_rmsnorm_workspace_size")
-            ws = workspace if workspace is not None else hidden.new_empty(need, dtype=torch.uint8)
+            ws = _space(workspace, hidden, need)
         _call("lce_add_rmsnorm_backward", dev, grad_normed.data_ptr(), _pitch(grad_normed, "grad_normed"),
               *_optional(grad_added, "grad_added"), hidden.data_ptr(), _pitch(hidden, "hidden"),
-              *_optional(residual, "residual"), gamma.data_ptr(), rstd.data_ptr(), N, H, DTYPES[hidden.dtype],
+              *_optional(residual, "residual"), gamma.data_ptr(), rstd.data_ptr(), N, H, DTYPES[dtype],
               dx.data_ptr(), _pitch(dx, "grad_hidden"), None if dg is None else dg.data_ptr(),
               None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())
     return dx, dg
@@ -339,12 +347,6 @@ def grad_norm_workspace_size(count: int) -> int:
     return int((_lib or _library()).lce_grad_norm_workspace_size(count))
 
 
-def _grad_workspace(workspace, grads):
-    if workspace is not None:
-        return workspace
-    return grads[0].new_empty(grad_norm_workspace_size(len(grads)), dtype=torch.uint8)
-
-
 def grad_norm(grads, norm_type: float = 2.0, workspace: torch.Tensor | None = None):
     """The norm (2 or inf) over all values of the gradients: a device scalar in fp32, squares summed in fp64.
 
@@ -354,14 +356,14 @@ def grad_norm(grads, norm_type: float = 2.0, workspace: torch.Tensor | None = No
     kind = _norm_type(norm_type)
     grads, dev, table = _check_grads(grads)
     norm = grads[0].new_empty((), dtype=torch.float32)
-    ws = _grad_workspace(workspace, grads)
+    ws = _space(workspace, grads[0], grad_norm_workspace_size(len(grads)))
     _call("lce_grad_norm", dev, table.buffer_info()[0], len(grads), kind, norm.data_ptr(), ws.data_ptr(), ws.numel())
     return norm
 
 
 def _clip(grads, dev, table, max_norm, norm_type, out, workspace):
     norm = grads[0].new_empty((), dtype=torch.float32)
-    ws = _grad_workspace(workspace, grads)
+    ws = _space(workspace, grads[0], grad_norm_workspace_size(len(grads)))
     outs = None if out is None else array.array("Q", [t.data_ptr() for t in out])
     _written(grads if out is None else out)
     _call("lce_clip_grad_norm", dev, table.buffer_info()[0], len(grads), norm_type, max_norm,

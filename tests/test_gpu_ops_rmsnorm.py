@@ -84,6 +84,23 @@ def test_many_rows(lce):
         _check_forward(*lce.add_rmsnorm_forward(x, r, gamma, EPS, return_rstd=True), x, r, gamma)
 
 
+def test_more_rows_than_a_grid(lce):
+    """17 million rows of 8 values: more than one workgroup for 16 rows allows, so the kernel walks on; rows after
+    the last one stay."""
+    N, H = 17_000_003, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((N, H), generator=g, device="cuda").to(torch.bfloat16)
+    gamma = (1 + 0.1 * torch.randn(H, generator=g, device="cuda")).to(torch.bfloat16)
+    out = torch.full((N + 50, H), 5.0, dtype=torch.bfloat16, device="cuda")
+    lce.add_rmsnorm_forward(x, None, gamma, EPS, normed=out[:N])
+    assert bool((out[N:] == 5).all())
+    for at in (slice(0, 4000), slice((1 << 24) - 2000, (1 << 24) + 2000), slice(N - 4000, N)):
+        _check_forward(out[at], None, None, x[at], None, gamma)
+    want = x.double() * (x.double().square().mean(1, keepdim=True) + EPS).rsqrt() * gamma.double()
+    # Within one step of bfloat16 (2^-7) everywhere; most exactly its rounding.
+    assert bool(((out[:N].double() - want).abs() <= 2.0 ** -8 * 1.001 * want.abs()).all())
+
+
 def test_no_rows(lce):
     x, r, gamma, _, _ = _inputs(1, 64, "bf16")
     x, r = x[:0], r[:0]
@@ -363,6 +380,9 @@ def test_refusals(lce):
         with pytest.raises(lce.LCEError) as e:
             call()
         assert e.value.status == status
+    for space in (torch.empty(1 << 22, dtype=torch.uint8), torch.empty(1 << 22, dtype=torch.float32, device="cuda")):
+        with pytest.raises(ValueError):
+            lce.add_rmsnorm_backward(dy, ds, x, r, gamma, rstd, workspace=space)
     wide = torch.zeros(1, 32776, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(lce.LCEError) as e:
         lce.rmsnorm(wide, wide[0])
@@ -407,3 +427,32 @@ def test_streams_and_graphs(lce):
         x.mul_(0.75)
         want = [t.clone() for t in everything(spaces[0])]
         torch.cuda.synchronize()
+
+
+def test_autograd_in_a_graph(lce):
+    """The forward and the gradients captured together, replayed on inputs changed in place."""
+    x, r, gamma, dy, ds = _inputs(100, 520, "bf16", seed=12)
+    leaves = [t.requires_grad_() for t in (x, r, gamma)]
+
+    def step():
+        return torch.autograd.grad(lce.add_rmsnorm(*leaves, EPS), leaves, (dy, ds))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = step()
+    for k in range(4):
+        with torch.no_grad():
+            x.mul_(1.25)
+        want = [t.clone() for t in step()]
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), k

@@ -84,7 +84,7 @@ def _backward(lib, **kw):
     (dict(dy=None), INVALID), (dict(x=None), INVALID), (dict(g=None), INVALID), (dict(rstd=None), INVALID),
     (dict(dx=None), INVALID), (dict(N=-1), INVALID), (dict(H=0), INVALID), (dict(dtype=9), INVALID),
     (dict(dy_ld=-4), INVALID), (dict(dx_ld=60), INVALID), (dict(H=40000), UNSUPPORTED), (dict(ws=None), WS_SMALL),
-    (dict(wsb=8), WS_SMALL), (dict(dx=DY + 2), INVALID), (dict(dx=X, dx_ld=72), INVALID), (dict(dx=R - 2), INVALID), (dict(dx=G, N=1), INVALID), (dict(dg=G), INVALID),
+    (dict(wsb=8), WS_SMALL), (dict(ws=WS + 64), INVALID), (dict(dx=DY + 2), INVALID), (dict(dx=X, dx_ld=72), INVALID), (dict(dx=R - 2), INVALID), (dict(dx=G, N=1), INVALID), (dict(dg=G), INVALID),
     (dict(dg=DX), INVALID), (dict(dx=RS), INVALID), (dict(N=0, dg=None), OK), (dict(N=0, dg=None, ws=None), OK),
 ])
 def test_backward_validation(lib, kw, status):
@@ -121,6 +121,7 @@ def test_clip_validation(lib):
     assert _clip(lib, _list(a), max_norm=-1.0) == INVALID and _clip(lib, _list(a), max_norm=float("nan")) == INVALID
     assert _clip(lib, _list((None, 1, BF16))) == INVALID and _clip(lib, _list((X, -1, BF16))) == INVALID
     assert _clip(lib, _list((X, 1, 3))) == INVALID
+    assert _clip(lib, _list(a), ws=WS + 8) == INVALID
     assert _clip(lib, _list(a), ws=None) == WS_SMALL and _clip(lib, _list(a), wsb=64) == WS_SMALL
     assert _clip(lib, _list(*[(X + 512 * k, 100, BF16) for k in range(300)]),
                  wsb=lib.lce_grad_norm_workspace_size(112)) == WS_SMALL
