@@ -114,7 +114,9 @@ lce_status_t run_forward(const NormArgs& a, hipStream_t s) {
   by_width(a.H, [&](auto tpr, auto ch) {
     constexpr int kTpr = decltype(tpr)::value, kCh = decltype(ch)::value, kThreads = threads_of(kTpr);
     const int64_t blocks = std::min(cdiv(a.N, kThreads / kTpr), kForwardBlocks);
-    auto kernel = a.H % kNormVec == 0 ? add_rmsnorm_kernel<T, kTpr, kCh, QUANT, true> : add_rmsnorm_kernel<T, kTpr, kCh, QUANT, false>;
+    auto kernel = a.H % kNormVec == 0 ? add_rmsnorm_kernel<T, kTpr, kCh, QUANT, WHOLE> : add_rmsnorm_kernel<T, kTpr, kCh, QUANT, PART>;
+    if constexpr (kTpr == 16)
+      if (a.H < kNormVec) kernel = add_rmsnorm_kernel<T, kTpr, kCh, QUANT, TINY>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, s, a);
   });
   return launched();
@@ -126,8 +128,10 @@ lce_status_t run_backward(const NormBackwardArgs& a, int64_t blocks, void* dgamm
     by_width(a.H, [&](auto tpr, auto ch) {
       constexpr int kTpr = decltype(tpr)::value, kCh = decltype(ch)::value;
       constexpr bool kAhead = kTpr < 512 || (kTpr == 512 && (kCh < 4 || sizeof(T) == 2));  // as registers allow
-      auto kernel = a.H % kNormVec == 0 ? add_rmsnorm_backward_kernel<T, kTpr, kCh, true, kAhead>
-                                        : add_rmsnorm_backward_kernel<T, kTpr, kCh, false, false>;
+      auto kernel = a.H % kNormVec == 0 ? add_rmsnorm_backward_kernel<T, kTpr, kCh, WHOLE, kAhead>
+                                        : add_rmsnorm_backward_kernel<T, kTpr, kCh, PART, kAhead>;
+      if constexpr (kTpr == 16)
+        if (a.H < kNormVec) kernel = add_rmsnorm_backward_kernel<T, kTpr, kCh, TINY, kAhead>;
       hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(threads_of(kTpr)), 0, s, a);
     });
   if (dgamma != nullptr)

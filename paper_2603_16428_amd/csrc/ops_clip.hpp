@@ -47,28 +47,34 @@ __device__ __forceinline__ double block_join(double v, double* lds) {
   return join<INF>(join<INF>(lds[0], lds[1]), join<INF>(lds[2], lds[3]));
 }
 
-// One piece's share of the norm: kVec values per thread and step, all four steps requested at once.
+// One piece's share of the norm: kVec values per thread and step, all four steps requested at once. A tensor's
+// last piece ends with up to kVec - 1 values that go one by one.
 template <typename T, bool INF>
 __device__ __forceinline__ double piece_norm(const T* p, int64_t n, double acc) {
-  constexpr int kVec = 16 / (int)sizeof(T), kSteps = kPieceBytes / 16 / kGradThreads;
+  constexpr int kVec = 16 / (int)sizeof(T), kSteps = kPieceBytes / 16 / kGradThreads, kAll = kPieceBytes / (int)sizeof(T);
   T raw[kSteps][kVec];
   double part[2] = {acc, 0.0};
-  if (n >= kPieceBytes / (int)sizeof(T)) {
+  auto add = [&](T x, int to) {
+    const double v = (double)to_f32(x);
+    part[to] = INF ? max_nan(part[to], fabs(v)) : fma(v, v, part[to]);
+  };
+  if (n >= kAll) {
 #pragma unroll
     for (int u = 0; u < kSteps; ++u) __builtin_memcpy(raw[u], p + (u * kGradThreads + threadIdx.x) * kVec, 16);
-#pragma unroll
-    for (int u = 0; u < kSteps; ++u)
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        const double v = (double)to_f32(raw[u][e]);
-        part[e & 1] = INF ? max_nan(part[e & 1], fabs(v)) : fma(v, v, part[e & 1]);
-      }
   } else {
-    for (int64_t k = threadIdx.x; k < n; k += kGradThreads) {
-      const double v = (double)to_f32(p[k]);
-      part[0] = INF ? max_nan(part[0], fabs(v)) : fma(v, v, part[0]);
+#pragma unroll
+    for (int u = 0; u < kSteps; ++u) {
+      const int at = (u * kGradThreads + threadIdx.x) * kVec;
+      __builtin_memset(raw[u], 0, 16);
+      if (at + kVec <= n) __builtin_memcpy(raw[u], p + at, 16);
     }
+    const int at = (int)n / kVec * kVec + (int)threadIdx.x;
+    if (at < n) add(p[at], 0);
   }
+#pragma unroll
+  for (int u = 0; u < kSteps; ++u)
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) add(raw[u][e], e & 1);
   return join<INF>(part[0], part[1]);
 }
 
@@ -78,21 +84,28 @@ __device__ __forceinline__ double piece_norm(const T* p, int64_t n, double acc) 
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
 template <typename T>
 __device__ __forceinline__ void piece_scale(const T* p, T* out, int64_t n, float f) {
-  constexpr int kVec = 16 / (int)sizeof(T), kSteps = kPieceBytes / 16 / kGradThreads;
+  constexpr int kVec = 16 / (int)sizeof(T), kSteps = kPieceBytes / 16 / kGradThreads, kAll = kPieceBytes / (int)sizeof(T);
   T raw[kSteps][kVec];
-  if (n >= kPieceBytes / (int)sizeof(T)) {
+  const bool all = n >= kAll;
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) __builtin_memcpy(raw[u], p + (u * kGradThreads + threadIdx.x) * kVec, 16);
+  for (int u = 0; u < kSteps; ++u) {
+    const int at = (u * kGradThreads + threadIdx.x) * kVec;
+    if (all || at + kVec <= n) __builtin_memcpy(raw[u], p + at, 16);
+  }
 #pragma unroll
-    for (int u = 0; u < kSteps; ++u) {
+  for (int u = 0; u < kSteps; ++u) {
+    const int at = (u * kGradThreads + threadIdx.x) * kVec;
+    if (all || at + kVec <= n) {
 #pragma unroll
       for (int e = 0; e < kVec; ++e) raw[u][e] = from_f32<T>(to_f32(raw[u][e]) * f);
       u32x4 w;
       __builtin_memcpy(&w, raw[u], 16);
-      __builtin_nontemporal_store(w, (u32x4_any*)(out + (u * kGradThreads + threadIdx.x) * kVec));
+      __builtin_nontemporal_store(w, (u32x4_any*)(out + at));
     }
-  } else {
-    for (int64_t k = threadIdx.x; k < n; k += kGradThreads) out[k] = from_f32<T>(to_f32(p[k]) * f);
+  }
+  if (!all) {
+    const int at = (int)n / kVec * kVec + (int)threadIdx.x;
+    if (at < n) out[at] = from_f32<T>(to_f32(p[at]) * f);
   }
 }
 
@@ -148,11 +161,11 @@ __device__ __forceinline__ void norm_pieces(const TensorEntry* e, const GradRun&
 }
 
 template <bool INF>
-__global__ __launch_bounds__(kGradThreads) void grad_norm_kernel(const TensorTable t, const GradRun r, double* __restrict__ part) {
+__global__ __launch_bounds__(kGradThreads, 8) void grad_norm_kernel(const TensorTable t, const GradRun r, double* __restrict__ part) {
   norm_pieces<INF>(t.entry, r, part);
 }
 template <bool INF>
-__global__ __launch_bounds__(kGradThreads) void grad_norm_many_kernel(const TensorEntry* __restrict__ e, const GradRun r,
+__global__ __launch_bounds__(kGradThreads, 8) void grad_norm_many_kernel(const TensorEntry* __restrict__ e, const GradRun r,
                                                                       double* __restrict__ part) {
   norm_pieces<INF>(e, r, part);
 }
@@ -209,7 +222,7 @@ __device__ __forceinline__ void clip_pieces(const TensorEntry* e, const GradRun&
 }
 
 template <bool INF>
-__global__ __launch_bounds__(kGradThreads) void clip_kernel(const TensorTable t, const GradRun r, const ClipArgs a) {
+__global__ __launch_bounds__(kGradThreads, 8) void clip_kernel(const TensorTable t, const GradRun r, const ClipArgs a) {
   clip_pieces<INF>(t.entry, r, a);
 }
 template <bool INF>

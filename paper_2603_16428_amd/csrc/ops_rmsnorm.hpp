@@ -30,39 +30,63 @@ struct RawRow {
       return (float)__builtin_bit_cast(f16, (uint16_t)(e & 1 ? w[e / 2] >> 16 : w[e / 2]));
     }
   }
-  __device__ __forceinline__ void keep_if(bool yes) {
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-    for (uint32_t& v : w) v = yes ? v : 0u;
+    for (uint32_t& v : w) v = 0u;
+  }
+  // Drops the first `d` values (1 to 7) and fills up with zeros.
+  __device__ __forceinline__ void drop(int d) {
+    constexpr int kW = kNormVec * sizeof(T) / 4;
+    auto words = [&](int by) {
+#pragma unroll
+      for (int k = 0; k < kW; ++k) w[k] = k + by < kW ? w[k + by] : 0u;
+    };
+    if (d & 4) words(kW / 2);
+    if (d & 2) words(kW / 4);
+    if (d & 1) {
+      if constexpr (sizeof(T) == 4) {
+        words(1);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kW; ++k) w[k] = w[k] >> 16 | (k + 1 < kW ? w[k + 1] << 16 : 0u);
+      }
+    }
   }
 };
-// The values from column c on, of which the first n exist (the others are 0; n may be <= 0). WHOLE: H is a
-// multiple of 8, so a thread's 8 values exist or not: they are loaded without a branch (from column `whole`,
-// which exists for every thread) and the caller masks what it must. A branch per load keeps the compiler
-// from requesting them together (backward in bf16, 8192 x 4096: 113 us, and 65 without).
-template <bool WHOLE, typename T>
-__device__ __forceinline__ void load_raw(const T* row, int c, int whole, int n, RawRow<T>& raw) {
-  if constexpr (WHOLE) {
-    __builtin_memcpy(raw.w, row + whole, sizeof(raw.w));
-  } else {
+// How rows end. WHOLE: H is a multiple of 8, so a thread's 8 values all exist or none does. PART: a row's last
+// values are loaded as the 8 that end the row, and align_end moves them into place, so that they, too, are one
+// load that nothing waits for. (Loaded one by one behind a branch they keep the compiler from requesting several
+// rows' values together: backward of 8192 x 4097 in bf16 218 us, 95 so, 69 where rows begin at
+// 4 bytes.) TINY: H < 8, value by value.
+enum RowEnd { WHOLE = 0, PART = 1, TINY = 2 };
+
+// The values at p, of which the first n exist (n <= 0: the registers stay as they are).
+template <RowEnd END, typename T>
+__device__ __forceinline__ void load_raw(const T* p, int n, RawRow<T>& raw) {
+  if constexpr (END == TINY) {
     T v[kNormVec];
-    if (n >= kNormVec) {
-      __builtin_memcpy(v, row + c, sizeof(v));
-    } else {
 #pragma unroll
-      for (int e = 0; e < kNormVec; ++e) v[e] = e < n ? row[c + e] : (T)0.f;
-    }
+    for (int e = 0; e < kNormVec; ++e) v[e] = e < n ? p[e] : (T)0.f;
     __builtin_memcpy(raw.w, v, sizeof(v));
+  } else if (n > 0) {
+    __builtin_memcpy(raw.w, END == WHOLE ? p : p + min(0, n - kNormVec), sizeof(raw.w));
+  }
+}
+template <RowEnd END, typename... Raw>
+__device__ __forceinline__ void align_end(int n, Raw&... raw) {
+  if constexpr (END == PART) {
+    if (n > 0 && n < kNormVec) (raw.drop(kNormVec - n), ...);
   }
 }
 
-template <bool WHOLE = false, typename T>
+template <RowEnd END, typename T>
 __device__ __forceinline__ void store_row(T* p, int n, const float (&v)[kNormVec]) {
   if (n >= kNormVec) {
     T raw[kNormVec];
 #pragma unroll
     for (int e = 0; e < kNormVec; ++e) raw[e] = from_f32<T>(v[e]);
     __builtin_memcpy(p, raw, sizeof(raw));
-  } else if constexpr (!WHOLE) {
+  } else if constexpr (END != WHOLE) {
 #pragma unroll
     for (int e = 0; e < kNormVec; ++e)
       if (e < n) p[e] = from_f32<T>(v[e]);
@@ -71,7 +95,7 @@ __device__ __forceinline__ void store_row(T* p, int n, const float (&v)[kNormVec
 
 // 8 values in e4m3, to nearest even. All are NaN or at most 448 (up to an fp32 rounding, which goes to
 // 448): nothing has to be clamped.
-template <bool WHOLE>
+template <RowEnd END>
 __device__ __forceinline__ void store_row_fp8(uint8_t* p, int n, const float (&v)[kNormVec]) {
   uint32_t w[2];
 #pragma unroll
@@ -81,7 +105,7 @@ __device__ __forceinline__ void store_row_fp8(uint8_t* p, int n, const float (&v
   }
   if (n >= kNormVec) {
     __builtin_memcpy(p, w, 8);
-  } else if constexpr (!WHOLE) {
+  } else if constexpr (END != WHOLE) {
 #pragma unroll
     for (int e = 0; e < kNormVec; ++e)
       if (e < n) p[e] = (uint8_t)(w[e / 4] >> (8 * (e % 4)));
@@ -123,7 +147,7 @@ struct NormArgs {
 constexpr float kFp8Max = 448.f;
 constexpr float kScaleMin = 1.17549435e-38f;  // 2^-126, whose inverse is still finite
 
-template <typename T, int TPR, int CH, bool QUANT, bool WHOLE>
+template <typename T, int TPR, int CH, bool QUANT, RowEnd END>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(const NormArgs a) {
   constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR, kWaves = TPR > 64 ? TPR / 64 : 1;
   __shared__ float sums[2][kWaves];
@@ -134,34 +158,26 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
   for (int64_t base = (int64_t)blockIdx.x * kRows; base < a.N; base += (int64_t)gridDim.x * kRows, turn ^= 1) {
     const int64_t i = base + threadIdx.x / TPR;
     const bool live = i < a.N;
-    const int64_t row = live ? i : a.N - 1;
+    const T *px = (const T*)a.x + i * a.x_ld, *pres = (const T*)a.residual + i * a.residual_ld;
     RawRow<T> x[CH], res[CH], gamma[CH];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TPR + t) * kNormVec;
-      load_raw<WHOLE>((const T*)a.x + row * a.x_ld, c, min(c, a.H - kNormVec), live ? a.H - c : 0, x[k]);
-      res[k].keep_if(false);
-    }
-    if (a.residual != nullptr) {
-#pragma unroll
-      for (int k = 0; k < CH; ++k) {
-        const int c = (k * TPR + t) * kNormVec;
-        load_raw<WHOLE>((const T*)a.residual + row * a.residual_ld, c, min(c, a.H - kNormVec), live ? a.H - c : 0, res[k]);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-      const int c = (k * TPR + t) * kNormVec;
-      load_raw<WHOLE>((const T*)a.gamma, c, min(c, a.H - kNormVec), a.H - c, gamma[k]);
+      const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
+      x[k].clear();
+      res[k].clear();
+      gamma[k].clear();
+      load_raw<END>(px + c, n, x[k]);
+      if (a.residual != nullptr) load_raw<END>(pres + c, n, res[k]);
+      load_raw<END>((const T*)a.gamma + c, n, gamma[k]);
     }
     float s[CH][kNormVec];
     float ss = 0.f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const bool mine = !WHOLE || (live && (k * TPR + t) * kNormVec < a.H);
+      align_end<END>(live ? a.H - (k * TPR + t) * kNormVec : 0, x[k], res[k], gamma[k]);
 #pragma unroll
       for (int e = 0; e < kNormVec; ++e) {
-        s[k][e] = mine ? x[k].at(e) + res[k].at(e) : 0.f;
+        s[k][e] = x[k].at(e) + res[k].at(e);
         ss = fmaf(s[k][e], s[k][e], ss);
       }
     }
@@ -172,11 +188,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
-      if (a.added != nullptr) store_row<WHOLE>((T*)a.added + i * a.added_ld + c, n, s[k]);
+      if (a.added != nullptr) store_row<END>((T*)a.added + i * a.added_ld + c, n, s[k]);
 #pragma unroll
       for (int e = 0; e < kNormVec; ++e) s[k][e] = s[k][e] * r * gamma[k].at(e);
       if constexpr (!QUANT) {
-        store_row<WHOLE>((T*)a.normed + i * a.normed_ld + c, n, s[k]);
+        store_row<END>((T*)a.normed + i * a.normed_ld + c, n, s[k]);
       } else {
         // The largest magnitude by its bits, among which a NaN's are above all others.
         uint32_t m = 0;
@@ -192,7 +208,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
             a.scales[i * ((a.H + a.group - 1) / a.group) + c / a.group] = scale < kScaleMin ? kScaleMin : scale;
 #pragma unroll
           for (int e = 0; e < kNormVec; ++e) s[k][e] *= inv;
-          store_row_fp8<WHOLE>((uint8_t*)a.normed + i * a.normed_ld + c, n, s[k]);
+          store_row_fp8<END>((uint8_t*)a.normed + i * a.normed_ld + c, n, s[k]);
         }
       }
     }
@@ -207,7 +223,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
           const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
 #pragma unroll
           for (int e = 0; e < kNormVec; ++e) s[k][e] *= inv;
-          store_row_fp8<WHOLE>((uint8_t*)a.normed + i * a.normed_ld + c, n, s[k]);
+          store_row_fp8<END>((uint8_t*)a.normed + i * a.normed_ld + c, n, s[k]);
         }
       }
     }
@@ -230,7 +246,7 @@ struct NormBackwardArgs {
 // Bound by HBM, so the loads may not stop while a row is reduced: AHEAD requests the next row's values
 // before the current one's dot product is joined. (A row's barrier and its joins take as long as its
 // loads.) What waits in registers waits in the input type.
-template <typename T, int TPR, int CH, bool WHOLE, bool AHEAD>
+template <typename T, int TPR, int CH, RowEnd END, bool AHEAD>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_kernel(const NormBackwardArgs a) {
   constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR, kWaves = TPR > 64 ? TPR / 64 : 1;
   constexpr int kCols = TPR * CH * kNormVec;
@@ -244,46 +260,40 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_ke
   __shared__ f32x4 wide_acc[kWide ? CH * 2 * TPR : 1];
   float acc[kWide ? 1 : CH][kNormVec];
   RawRow<T> g[kWide ? 1 : CH], x[CH], res[CH], dy[CH], ds[CH];
-  int whole[CH];
 #pragma unroll
   for (int k = 0; k < CH; ++k) {
     const int c = (k * TPR + t) * kNormVec;
-    whole[k] = min(c, a.H - kNormVec);
+    // Columns past the row's end are 0 in registers from here on and add nothing to any sum.
+    x[k].clear();
+    res[k].clear();
+    dy[k].clear();
+    ds[k].clear();
     if constexpr (kWide) {
       wide_acc[2 * k * TPR + t] = wide_acc[(2 * k + 1) * TPR + t] = (f32x4){};
     } else {
-      load_raw<WHOLE>((const T*)a.gamma, c, whole[k], a.H - c, g[k]);
+      g[k].clear();
+      load_raw<END>((const T*)a.gamma + c, a.H - c, g[k]);
+      align_end<END>(a.H - c, g[k]);
 #pragma unroll
       for (int e = 0; e < kNormVec; ++e) acc[k][e] = 0.f;
     }
-    res[k].keep_if(false);
-    ds[k].keep_if(false);
   }
   const int64_t stride = (int64_t)gridDim.x * kRows;
   float r = 0.f;
+  // The last rows' workgroup may have threads without a row: they take the last one again, and leave its
+  // gradients out.
   auto request = [&](int64_t i) {
-    const bool live = i < a.N;
-    const int64_t row = live ? i : a.N - 1;
+    const int64_t row = min(i, a.N - 1);
     r = a.rstd[row];
+    const T *pdy = (const T*)a.dy + row * a.dy_ld, *px = (const T*)a.x + row * a.x_ld;
+    const T *pres = (const T*)a.residual + row * a.residual_ld, *pds = (const T*)a.ds + row * a.ds_ld;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
-      load_raw<WHOLE>((const T*)a.dy + row * a.dy_ld, c, whole[k], n, dy[k]);
-      load_raw<WHOLE>((const T*)a.x + row * a.x_ld, c, whole[k], n, x[k]);
-    }
-    if (has_res) {
-#pragma unroll
-      for (int k = 0; k < CH; ++k) {
-        const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
-        load_raw<WHOLE>((const T*)a.residual + row * a.residual_ld, c, whole[k], n, res[k]);
-      }
-    }
-    if (has_ds) {
-#pragma unroll
-      for (int k = 0; k < CH; ++k) {
-        const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
-        load_raw<WHOLE>((const T*)a.ds + row * a.ds_ld, c, whole[k], n, ds[k]);
-      }
+      const int c = (k * TPR + t) * kNormVec, n = a.H - c;
+      load_raw<END>(pdy + c, n, dy[k]);
+      load_raw<END>(px + c, n, x[k]);
+      if (has_res) load_raw<END>(pres + c, n, res[k]);
+      if (has_ds) load_raw<END>(pds + c, n, ds[k]);
     }
   };
   int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
@@ -298,16 +308,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_ke
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       const int c = (k * TPR + t) * kNormVec;
+      align_end<END>(a.H - c, dy[k], x[k], res[k], ds[k]);
       dyi[k] = dy[k];
       dsi[k] = ds[k];
-      // What is not there adds nothing to a sum (nor does what another row in place is just writing there).
-      const bool mine = !WHOLE || (i < a.N && c < a.H);
-      dyi[k].keep_if(mine);
       RawRow<T>& gk = g[kWide ? 0 : k];
-      if (kWide) load_raw<WHOLE>((const T*)a.gamma, c, whole[k], a.H - c, gk);
+      if (kWide) {
+        gk.clear();
+        load_raw<END>((const T*)a.gamma + c, a.H - c, gk);
+        align_end<END>(a.H - c, gk);
+      }
 #pragma unroll
       for (int e = 0; e < kNormVec; ++e) {
-        s[k][e] = mine ? x[k].at(e) + res[k].at(e) : 0.f;
+        s[k][e] = x[k].at(e) + res[k].at(e);
         dot = fmaf(dyi[k].at(e) * gk.at(e), s[k][e], dot);
       }
     }
@@ -319,15 +331,25 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_ke
       const int c = (k * TPR + t) * kNormVec, n = i < a.N ? a.H - c : 0;
       float dx[kNormVec];
       RawRow<T>& gk = g[kWide ? 0 : k];
-      if (kWide) load_raw<WHOLE>((const T*)a.gamma, c, whole[k], a.H - c, gk);
+      if (kWide) {
+        gk.clear();
+        load_raw<END>((const T*)a.gamma + c, a.H - c, gk);
+        align_end<END>(a.H - c, gk);
+      }
+      if (kRows == 1 || i < a.N) {
+#pragma unroll
+        for (int e = 0; e < kNormVec; ++e) {
+          const float dg = dyi[k].at(e) * (s[k][e] * ri);
+          if constexpr (kWide) ((float*)&wide_acc[(2 * k + e / 4) * TPR + t])[e % 4] += dg;
+          else acc[k][e] += dg;
+        }
+      }
 #pragma unroll
       for (int e = 0; e < kNormVec; ++e) {
-        const float d = dyi[k].at(e), dg = d * (s[k][e] * ri);
-        if constexpr (kWide) ((float*)&wide_acc[(2 * k + e / 4) * TPR + t])[e % 4] += dg;
-        else acc[k][e] += dg;
+        const float d = dyi[k].at(e);
         dx[e] = fmaf(ri, d * gk.at(e) - s[k][e] * c1, dsi[k].at(e));
       }
-      store_row<WHOLE>((T*)a.dx + i * a.dx_ld + c, n, dx);
+      store_row<END>((T*)a.dx + i * a.dx_ld + c, n, dx);
     }
   }
   if (a.part == nullptr) return;
@@ -340,7 +362,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_ke
 #pragma unroll
         for (int e = 0; e < kNormVec; ++e) acc[0][e] = wide_acc[(2 * k + e / 4) * TPR + t][e % 4];
       }
-      store_row<WHOLE>(out + c, a.H - c, acc[kWide ? 0 : k]);
+      store_row<END>(out + c, a.H - c, acc[kWide ? 0 : k]);
     }
   } else {
     __shared__ float cols[kRows][kCols];

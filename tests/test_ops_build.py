@@ -1,6 +1,5 @@
-"""Build invariants of the operators' kernels, from the compiler's own report: rows up to 16384 values are held
-in registers (no scratch memory, except the backward's widest fp32 variant), occupancy as the launch counts on,
-and no packed fp32 arithmetic."""
+"""Build invariants of the operators' kernels, from the compiler's own report: rows of up to 16384 values are held
+in registers (no scratch memory), occupancy as the launch counts on, and no packed fp32 arithmetic."""
 import os
 import re
 import subprocess
@@ -41,19 +40,19 @@ def test_rows_are_in_registers(report):
             continue
         seen += 1
         backward, dtype, threads, steps = n
-        if threads == 1024 or (backward and dtype == "f" and threads == 512):
-            continue
-        assert use["ScratchSize"] == 0, (name, use)
-    assert seen == 2 * 3 * 10 * 2 + 3 * 10 * 2
+        assert use["ScratchSize"] == 0 or threads == 1024, (name, use)
+    # Ten widths, each with rows that end in whole and in part pieces, and the one for H < 8; three types; the
+    # forward in its own type and in e4m3, and the backward.
+    assert seen == (2 * 10 + 1) * 3 * 3
 
 
 def test_gradient_kernels_are_resident_at_once(report):
-    """2048 workgroups of 4 waves on 256 CUs of 4 SIMDs: 8 waves each."""
+    """2048 workgroups of 4 waves on 256 CUs of 4 SIMDs: 8 waves each (7 where clipping reads its table from memory)."""
     kernels, _ = report
     names = [n for n in kernels if re.search(r"\d(grad_norm_kernel|grad_norm_many_kernel|clip_kernel|clip_many_kernel)I", n)]
     assert len(names) == 8
     for n in names:
-        assert kernels[n]["Occupancy"] >= 8 and kernels[n]["ScratchSize"] == 0, (n, kernels[n])
+        assert kernels[n]["Occupancy"] >= (7 if "clip_many" in n else 8) and kernels[n]["ScratchSize"] == 0, (n, kernels[n])
 
 
 def test_no_packed_fp32(report):
