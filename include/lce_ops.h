@@ -7,7 +7,7 @@
  * Conventions are those of lce.h (device pointers owned by the caller, work enqueued in order on
  * `stream`, which belongs to the current device, no allocation and no synchronisation, arguments
  * validated before anything is enqueued, status codes, deterministic results), except:
- *   - Tensors need only their element type's alignment.
+ *   - Tensors need only their element type's alignment (any other gives LCE_ERR_INVALID_ARGUMENT).
  *   - Row tensors [N, H] have a pitch of their own (`*_ld`, elements between rows): any for an input,
  *     0 included (one row for all), at least H for an output. The H values of a row are consecutive.
  *   - N >= 0 (N = 0 does nothing), H from 1 to LCE_NORM_MAX_H, any values: rows need not be whole
@@ -30,7 +30,8 @@ extern "C" {
  * in fp32, each output rounded once to its type. The norm takes s before its rounding to `dtype`.
  *   x, residual : device [N,H] of dtype; residual may be NULL.
  *   gamma       : device [H] of dtype.
- *   eps         : >= 0 and finite. The mean square has to stay within fp32 (values below about 1e19).
+ *   eps         : >= 0 and finite. The mean square has to stay within fp32: values below about 1e19, and
+ *                 with eps = 0 above about 1e-18 (a row of zeros then gives NaN).
  *   normed      : device [N,H] of dtype.
  *   added       : device [N,H] of dtype, receives s; NULL where it is not wanted.
  *   rstd        : device fp32 [N], receives r (the backward needs it); NULL where it is not wanted.
@@ -53,7 +54,8 @@ lce_status_t lce_add_rmsnorm_forward(const void* x, int64_t x_ld, const void* re
  *   group      : 32, 64 or 128 values (the row's last group may be shorter), or 0: the whole row.
  *   quantised  : device bytes [N,H] (pitch in bytes).
  *   scales     : device fp32 [N, ceil(H / group)] ([N, 1] for group 0), row-major. NaN where its group
- *                holds a NaN (all of the group's values are NaN then).
+ *                holds a NaN (all of the group's values are NaN then), infinite where a value's magnitude
+ *                passes fp32.
  * quantised and scales overlap no other tensor of the call.
  */
 lce_status_t lce_add_rmsnorm_quant(const void* x, int64_t x_ld, const void* residual, int64_t residual_ld,

@@ -45,9 +45,10 @@ lce_status_t check_rows(int64_t N, int64_t H, int dtype) {
   if (N < 0 || H < 1 || !dtype_ok(dtype)) return LCE_ERR_INVALID_ARGUMENT;
   return N > kMaxRows || H > LCE_NORM_MAX_H ? LCE_ERR_UNSUPPORTED : LCE_OK;
 }
-lce_status_t check_pitch(const void* p, int64_t ld, int64_t least) {
+// Pitch and alignment of rows (`size`: bytes of an element).
+lce_status_t check_pitch(const void* p, int64_t ld, int64_t least, int64_t size) {
   if (p == nullptr) return LCE_OK;
-  if (ld < least) return LCE_ERR_INVALID_ARGUMENT;
+  if (ld < least || (intptr_t)p % size != 0) return LCE_ERR_INVALID_ARGUMENT;
   return ld > kMaxPitch ? LCE_ERR_UNSUPPORTED : LCE_OK;
 }
 
@@ -157,14 +158,17 @@ int64_t count_pieces(const lce_tensor_t* grads, int64_t count, std::vector<Tenso
   return pieces;
 }
 
-// Whether memory that a clip writes overlaps any other tensor of the call; out[k] may be grads[k].data.
-bool clip_overlaps(const std::vector<TensorEntry>& table) {
+// Whether memory that a clip writes (the norm and the workspace too) overlaps any other of the call; out[k] may
+// be grads[k].data.
+bool clip_overlaps(const std::vector<TensorEntry>& table, const float* norm, const void* workspace) {
   struct Range {
     uintptr_t lo, hi;
     bool written;
   };
   std::vector<Range> r;
-  r.reserve(2 * table.size());
+  r.reserve(2 * table.size() + 2);
+  r.push_back({(uintptr_t)norm, (uintptr_t)norm + sizeof(float), true});
+  r.push_back({(uintptr_t)workspace, (uintptr_t)workspace + lce_grad_norm_workspace_size((int64_t)table.size()), true});
   for (const TensorEntry& e : table) {
     const uintptr_t bytes = (uintptr_t)(e.n * size_of(e.dtype));
     if (bytes == 0) continue;
@@ -233,20 +237,22 @@ lce_status_t run_norm(const std::vector<TensorEntry>& table, int64_t pieces, boo
 
 lce_status_t grad_norm_call(const lce_tensor_t* grads, int64_t count, int norm_type, bool clip, float max_norm,
                             void* const* out, float* norm, void* workspace, size_t workspace_bytes, hipStream_t s) {
-  if (!grads || count < 1 || !norm || (norm_type != LCE_NORM_L2 && norm_type != LCE_NORM_INF) || !(max_norm >= 0.f))
+  if (!grads || count < 1 || !norm || (norm_type != LCE_NORM_L2 && norm_type != LCE_NORM_INF) || !(max_norm >= 0.f) ||
+      (uintptr_t)norm % sizeof(float) != 0)
     return LCE_ERR_INVALID_ARGUMENT;
   if (count > INT32_MAX) return LCE_ERR_UNSUPPORTED;
   for (int64_t k = 0; k < count; ++k) {
     if (grads[k].n < 0 || !dtype_ok(grads[k].dtype)) return LCE_ERR_INVALID_ARGUMENT;
     if (grads[k].n > 0 && (!grads[k].data || (out != nullptr && !out[k]))) return LCE_ERR_INVALID_ARGUMENT;
+    const uintptr_t bits = (uintptr_t)grads[k].data | (out != nullptr ? (uintptr_t)out[k] : 0);
+    if (bits % size_of(grads[k].dtype) != 0) return LCE_ERR_INVALID_ARGUMENT;
   }
   try {  // the host's own memory: no exception leaves a C entry
     std::vector<TensorEntry> table((size_t)count);
     const int64_t pieces = count_pieces(grads, count, table, out);
     if (pieces < 0) return LCE_ERR_UNSUPPORTED;
-    if (clip && clip_overlaps(table)) return LCE_ERR_INVALID_ARGUMENT;
     if (!workspace || workspace_bytes < lce_grad_norm_workspace_size(count)) return LCE_ERR_WORKSPACE_TOO_SMALL;
-    if ((uintptr_t)workspace % 256 != 0) return LCE_ERR_INVALID_ARGUMENT;
+    if ((uintptr_t)workspace % 256 != 0 || (clip && clip_overlaps(table, norm, workspace))) return LCE_ERR_INVALID_ARGUMENT;
     return norm_type == LCE_NORM_INF ? run_norm<true>(table, pieces, clip, out == nullptr, max_norm, norm, workspace, s)
                                      : run_norm<false>(table, pieces, clip, out == nullptr, max_norm, norm, workspace, s);
   } catch (...) {
@@ -264,10 +270,11 @@ lce_status_t forward_args(const void* x, int64_t x_ld, const void* residual, int
   if (!eps_ok(eps)) return LCE_ERR_INVALID_ARGUMENT;
   if (N == 0) return LCE_OK;
   if (!x || !gamma || !normed) return LCE_ERR_INVALID_ARGUMENT;
-  for (const lce_status_t e : {check_pitch(x, x_ld, 0), check_pitch(residual, residual_ld, 0),
-                               check_pitch(normed, normed_ld, H), check_pitch(added, added_ld, H)})
-    if (e != LCE_OK) return e;
   const int64_t z = size_of(dtype);
+  for (const lce_status_t e : {check_pitch(x, x_ld, 0, z), check_pitch(residual, residual_ld, 0, z), check_pitch(gamma, H, H, z),
+                               check_pitch(normed, normed_ld, H, normed_size), check_pitch(added, added_ld, H, z),
+                               check_pitch(rstd, 1, 1, 4), check_pitch(scales, groups, groups, 4)})
+    if (e != LCE_OK) return e;
   const bool quant = scales != nullptr;
   st = check_overlaps({{{normed, normed_ld * normed_size, H * normed_size, N}, !quant},
                        {{added, added_ld * z, H * z, N}, true},
@@ -331,11 +338,15 @@ lce_status_t lce_add_rmsnorm_backward(const void* grad_normed, int64_t grad_norm
   const int64_t z = lce::size_of(dtype);
   if (N > 0) {
     if (!grad_normed || !x || !gamma || !rstd || !grad_hidden) return LCE_ERR_INVALID_ARGUMENT;
-    for (const lce_status_t e : {lce::check_pitch(grad_normed, grad_normed_ld, 0), lce::check_pitch(grad_added, grad_added_ld, 0),
-                                 lce::check_pitch(x, x_ld, 0), lce::check_pitch(residual, residual_ld, 0),
-                                 lce::check_pitch(grad_hidden, grad_hidden_ld, H)})
+    for (const lce_status_t e :
+         {lce::check_pitch(grad_normed, grad_normed_ld, 0, z), lce::check_pitch(grad_added, grad_added_ld, 0, z),
+          lce::check_pitch(x, x_ld, 0, z), lce::check_pitch(residual, residual_ld, 0, z), lce::check_pitch(gamma, H, H, z),
+          lce::check_pitch(rstd, 1, 1, 4), lce::check_pitch(grad_hidden, grad_hidden_ld, H, z), lce::check_pitch(grad_gamma, H, H, z)})
       if (e != LCE_OK) return e;
-    st = lce::check_overlaps({{{grad_hidden, grad_hidden_ld * z, H * z, N}, true}, {{grad_gamma, H * z, H * z, 1}, false}},
+    const int64_t space = (int64_t)lce_add_rmsnorm_workspace_size(N, H, dtype);
+    st = lce::check_overlaps({{{grad_hidden, grad_hidden_ld * z, H * z, N}, true},
+                              {{grad_gamma, H * z, H * z, 1}, false},
+                              {{grad_gamma != nullptr ? workspace : nullptr, space, space, 1}, false}},
                              {{grad_normed, grad_normed_ld * z, H * z, N},
                               {grad_added, grad_added_ld * z, H * z, N},
                               {x, x_ld * z, H * z, N},

@@ -315,6 +315,53 @@ def test_autograd(lce, dtype):
         assert lce.add_rmsnorm_forward(a, b, gamma, EPS, normed=a, added=b)[0] is a
 
 
+def test_autograd_of_shared_and_broadcast_inputs(lce):
+    """One tensor as both addends, one row added to all, no rows, a single row."""
+    x, res, gamma, dy, ds = _inputs(30, 136, "fp32", seed=8)
+    a = x.clone().requires_grad_()
+    got, = torch.autograd.grad(lce.add_rmsnorm(a, a, gamma, EPS), a, (dy, ds))
+    _, s, r = lce.add_rmsnorm_forward(x, x, gamma, EPS, return_rstd=True)
+    dx, _ = lce.add_rmsnorm_backward(dy, ds, x, x, gamma, r)
+    assert torch.equal(got, dx + dx)
+    one = res[:1].clone().requires_grad_()
+    got, = torch.autograd.grad(lce.add_rmsnorm(x, one.expand(30, 136), gamma, EPS), one, (dy, ds))
+    _, s, r = O.add_rmsnorm(x, res[:1], gamma, EPS)
+    want, _ = O.add_rmsnorm_backward(dy, ds, s, gamma, r)
+    # Each row's gradient as in _check_backward (w for its rounding), and 30 fp32 additions of the rows.
+    f = [t.cpu().double().abs() for t in (dy, ds, s, gamma, r[:, None])]
+    rows = 8 * (f[4] * f[3] * f[0] + f[1]) + 64 * f[4] ** 3 * f[2] * (f[0] * f[3] * f[2]).mean(1, keepdim=True) + want.abs()
+    assert bool(((got[0].cpu().double() - want.sum(0)).abs() <= W * (rows.sum(0) + 30 * want.abs().sum(0))).all())
+    empty, g = x[:0].clone().requires_grad_(), gamma.clone().requires_grad_()
+    grads = torch.autograd.grad(lce.rmsnorm(empty, g, EPS).sum(), (empty, g))
+    assert grads[0].shape == (0, 136) and not grads[1].any()
+    row = x[0].clone().requires_grad_()
+    got = torch.autograd.grad(lce.rmsnorm(row, g, EPS), (row, g), dy[0])
+    _, s, r = lce.add_rmsnorm_forward(x[:1], None, gamma, EPS, return_rstd=True)
+    want = lce.add_rmsnorm_backward(dy[:1], None, x[:1], None, gamma, r)
+    assert torch.equal(got[0], want[0][0]) and torch.equal(got[1], want[1])
+
+
+def test_two_streams_at_once(lce):
+    """Calls on two streams that run at the same time, each with its own outputs and workspace."""
+    sets = [_inputs(2000, 4096, "bf16", seed=k) for k in (20, 21)]
+    want = []
+    for x, r, g, dy, ds in sets:
+        n, a, rs = lce.add_rmsnorm_forward(x, r, g, EPS, return_rstd=True)
+        want.append((n, a, *lce.add_rmsnorm_backward(dy, ds, x, r, g, rs), lce.grad_norm([n, a])))
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in sets], [[], []]
+    for _ in range(3):
+        for k, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                x, r, g, dy, ds = sets[k]
+                n, a, rs = lce.add_rmsnorm_forward(x, r, g, EPS, return_rstd=True)
+                got[k].append((n, a, *lce.add_rmsnorm_backward(dy, ds, x, r, g, rs), lce.grad_norm([n, a])))
+    torch.cuda.synchronize()
+    for k in range(2):
+        for outs in got[k]:
+            assert all(torch.equal(a, b) for a, b in zip(outs, want[k]))
+
+
 def test_gradients_are_the_forwards_differences(lce):
     """Along random directions, with the outputs' values in float64 from the formula: the derivative of
     <dy, normed> + <ds, added> by central differences (step 1e-6, whose own error is below 1e-8 of the terms)

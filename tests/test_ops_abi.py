@@ -48,6 +48,7 @@ ROWS = [
     (dict(dtype=3), INVALID), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID),
     (dict(x_ld=-1), INVALID), (dict(y_ld=63), INVALID), (dict(s_ld=63), INVALID), (dict(H=32769), UNSUPPORTED),
     (dict(N=1 << 31), UNSUPPORTED), (dict(x_ld=(1 << 30) + 1), UNSUPPORTED), (dict(N=0), OK), (dict(N=0, x=None), OK),
+    (dict(x=X + 1), INVALID), (dict(g=G + 1), INVALID), (dict(s=S + 1), INVALID), (dict(rstd=RS + 2), INVALID),
     # Outputs over inputs or over each other, partly or with another pitch.
     (dict(y=X + 16), INVALID), (dict(y=X, y_ld=72), INVALID), (dict(s=R + 2), INVALID), (dict(y=S), INVALID), (dict(y=G), INVALID), (dict(y=G, N=1), INVALID),
     (dict(rstd=X + 8), INVALID), (dict(rstd=Y + 4 * 128 - 4), INVALID), (dict(s=Y + 64), INVALID),
@@ -84,7 +85,8 @@ def _backward(lib, **kw):
     (dict(dy=None), INVALID), (dict(x=None), INVALID), (dict(g=None), INVALID), (dict(rstd=None), INVALID),
     (dict(dx=None), INVALID), (dict(N=-1), INVALID), (dict(H=0), INVALID), (dict(dtype=9), INVALID),
     (dict(dy_ld=-4), INVALID), (dict(dx_ld=60), INVALID), (dict(H=40000), UNSUPPORTED), (dict(ws=None), WS_SMALL),
-    (dict(wsb=8), WS_SMALL), (dict(ws=WS + 64), INVALID), (dict(dx=DY + 2), INVALID), (dict(dx=X, dx_ld=72), INVALID), (dict(dx=R - 2), INVALID), (dict(dx=G, N=1), INVALID), (dict(dg=G), INVALID),
+    (dict(wsb=8), WS_SMALL), (dict(ws=WS + 64), INVALID), (dict(ws=X), INVALID), (dict(ws=DX), INVALID), (dict(dy=DY + 1), INVALID),
+    (dict(rstd=RS + 1), INVALID), (dict(dg=DG + 1), INVALID), (dict(dx=DY + 2), INVALID), (dict(dx=X, dx_ld=72), INVALID), (dict(dx=R - 2), INVALID), (dict(dx=G, N=1), INVALID), (dict(dg=G), INVALID),
     (dict(dg=DX), INVALID), (dict(dx=RS), INVALID), (dict(N=0, dg=None), OK), (dict(N=0, dg=None, ws=None), OK),
 ])
 def test_backward_validation(lib, kw, status):
@@ -121,6 +123,9 @@ def test_clip_validation(lib):
     assert _clip(lib, _list(a), max_norm=-1.0) == INVALID and _clip(lib, _list(a), max_norm=float("nan")) == INVALID
     assert _clip(lib, _list((None, 1, BF16))) == INVALID and _clip(lib, _list((X, -1, BF16))) == INVALID
     assert _clip(lib, _list((X, 1, 3))) == INVALID
+    assert _clip(lib, _list((X + 1, 8, BF16))) == INVALID and _clip(lib, _list((X + 2, 8, FP32))) == INVALID
+    assert _clip(lib, _list(a), out=[Y + 1]) == INVALID and _clip(lib, _list(a), norm=SC + 2) == INVALID
+    assert _clip(lib, _list(a), norm=X + 196) == INVALID and _clip(lib, _list(a), ws=X - 256) == INVALID
     assert _clip(lib, _list(a), ws=WS + 8) == INVALID
     assert _clip(lib, _list(a), ws=None) == WS_SMALL and _clip(lib, _list(a), wsb=64) == WS_SMALL
     assert _clip(lib, _list(*[(X + 512 * k, 100, BF16) for k in range(300)]),
