@@ -217,26 +217,29 @@ def add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd,
     if rstd.shape != shape[:-1] or rstd.dtype != torch.float32 or rstd.device != dev or not rstd.is_contiguous():
         raise ValueError("rstd must be the forward call's")
     dx = _output(grad_hidden, hidden, dtype, "grad_hidden")
-    dg = torch.empty_like(gamma) if need_gamma else None
-    if N or need_gamma:
-        ws = None
-        if need_gamma:
-            need = (_lib or _library()).lce_add_rmsnorm_workspace_size(N, H, DTYPES[dtype])
-            if need == 0:
-                raise LCEError(2, "lce_add_rmsnorm_workspace_size")
-            ws = _space(workspace, hidden, need)
-        _call("lce_add_rmsnorm_backward", dev, grad_normed.data_ptr(), _pitch(grad_normed, "grad_normed"),
-              *_optional(grad_added, "grad_added"), hidden.data_ptr(), _pitch(hidden, "hidden"),
-              *_optional(residual, "residual"), gamma.data_ptr(), rstd.data_ptr(), N, H, DTYPES[dtype],
-              dx.data_ptr(), _pitch(dx, "grad_hidden"), None if dg is None else dg.data_ptr(),
-              None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel())
+    dg = ws = None
+    size = 0
+    if need_gamma:
+        dg = torch.empty_like(gamma)
+        size = (_lib or _library()).lce_add_rmsnorm_workspace_size(N, H, DTYPES[dtype])
+        if size == 0:
+            raise LCEError(2, "lce_add_rmsnorm_workspace_size")
+        ws = _space(workspace, hidden, size)
+        size = ws.numel()
+    elif N == 0:
+        return dx, None
+    _call("lce_add_rmsnorm_backward", dev, grad_normed.data_ptr(), _pitch(grad_normed, "grad_normed"),
+          *_optional(grad_added, "grad_added"), hidden.data_ptr(), _pitch(hidden, "hidden"),
+          *_optional(residual, "residual"), gamma.data_ptr(), rstd.data_ptr(), N, H, DTYPES[dtype],
+          dx.data_ptr(), _pitch(dx, "grad_hidden"), None if dg is None else dg.data_ptr(),
+          None if ws is None else ws.data_ptr(), size)
     return dx, dg
 
 
 def _upstream(g):
     """An upstream gradient as rows that the kernels can read: its values in memory, its rows evenly spaced."""
-    if g is None:
-        return None
+    if g is None or (type(g) is torch.Tensor and g.is_contiguous() and not g.is_neg() and g.data_ptr() != 0):
+        return g
     if not _bytes_are_values(g):
         if type(g) is not torch.Tensor:
             raise ValueError("the upstream gradient must be a plain tensor")
@@ -277,13 +280,14 @@ class AddRMSNorm(torch.autograd.Function):
     @staticmethod
     def _gradients(ctx, grad_normed, grad_added):
         hidden, residual, gamma, rstd = ctx.saved_tensors
-        need_gamma = ctx.needs_input_grad[2]
+        need = ctx.needs_input_grad
+        need_gamma = need[2]
         grad_normed, grad_added = _upstream(grad_normed), _upstream(grad_added)
         if grad_normed is None:  # nothing came back through the norm
             grads = grad_added, torch.zeros_like(gamma) if need_gamma else None
         else:
+            # All are checked again: hooks may have changed what was saved.
             grads = add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd, need_gamma)
-        need = ctx.needs_input_grad
         return grads[0] if need[0] else None, grads[0] if need[1] else None, grads[1], None
 
     _once = staticmethod(torch.autograd.function.once_differentiable(_gradients.__func__))

@@ -341,6 +341,21 @@ def test_autograd_of_shared_and_broadcast_inputs(lce):
     assert torch.equal(got[0], want[0][0]) and torch.equal(got[1], want[1])
 
 
+def test_hooks_that_change_what_was_saved(lce):
+    """Saved tensors that come back on the host, in another type or shape are refused; copies are fine."""
+    x, res, gamma, dy, ds = _inputs(5, 64, "bf16", seed=13)
+    leaves = [t.requires_grad_() for t in (x, res, gamma)]
+    want = torch.autograd.grad(lce.add_rmsnorm(*leaves, EPS), leaves, (dy, ds))
+    with torch.autograd.graph.save_on_cpu():
+        outs = lce.add_rmsnorm(*leaves, EPS)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(outs, leaves, (dy, ds)), want))
+    for change in (lambda t: t.cpu(), lambda t: t.double(), lambda t: t[..., :1], torch._neg_view):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, change):
+            outs = lce.add_rmsnorm(*leaves, EPS)
+        with pytest.raises(ValueError):
+            torch.autograd.grad(outs, leaves, (dy, ds))
+
+
 def test_two_streams_at_once(lce):
     """Calls on two streams that run at the same time, each with its own outputs and workspace."""
     sets = [_inputs(2000, 4096, "bf16", seed=k) for k in (20, 21)]
