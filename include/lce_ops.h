@@ -50,12 +50,11 @@ lce_status_t lce_add_rmsnorm_forward(const void* x, int64_t x_ld, const void* re
  *
  *     scale_ig = max(max_{j in g} |normed_ij| / 448, 2^-126),   quantised_ij = e4m3(normed_ij / scale_ig)
  *
- * from the fp32 values of normed (no rounding to dtype in between), to nearest even.
+ * from the unrounded values of normed, to nearest even.
  *   group      : 32, 64 or 128 values (the row's last group may be shorter), or 0: the whole row.
  *   quantised  : device bytes [N,H] (pitch in bytes).
- *   scales     : device fp32 [N, ceil(H / group)] ([N, 1] for group 0), row-major. NaN where its group
- *                holds a NaN (all of the group's values are NaN then), infinite where a value's magnitude
- *                passes fp32.
+ *   scales     : device fp32 [N, ceil(H / group)] ([N, 1] for group 0), row-major. Not
+ *                finite where its group holds a value that is not (its quantised values are NaN then).
  * quantised and scales overlap no other tensor of the call.
  */
 lce_status_t lce_add_rmsnorm_quant(const void* x, int64_t x_ld, const void* residual, int64_t residual_ld,

@@ -213,6 +213,21 @@ def test_quant(lce, H, group, dtype):
     _near(alone[1].view(N, -1), O.group_scales(O.add_rmsnorm(x, None, gamma, EPS)[0], group), 36 * W)
 
 
+def test_quant_at_the_smallest_scale(lce):
+    """Values around 2^-126 and below (a tiny gain): the scale stays at 2^-126, and fp32's own smallest step, 2^-149,
+    is what the arithmetic may be off (a few times)."""
+    x, r, gamma, _, _ = _inputs(7, 300, "fp32")
+    for group in (0, 32):
+        for size in (2.0 ** -122, 2.0 ** -130):
+            g = gamma * size
+            q, scales, _ = lce.add_rmsnorm_quant(x, r, g, EPS, group)
+            y, _, _ = O.add_rmsnorm(x, r, g, EPS)
+            assert bool((scales == O.SCALE_MIN).all())
+            off = (q.float().cpu().double() * O.SCALE_MIN - y).abs()
+            assert bool((off <= torch.clamp(2.0 ** -4 * y.abs(), min=2.0 ** -10 * O.SCALE_MIN) + 96 * W * y.abs() + 8 * 2.0 ** -149).all())
+            assert q.float().abs().max() > 0.1
+
+
 def test_quant_into_a_wider_buffer(lce):
     x, r, gamma, _, _ = _inputs(6, 300, "bf16")
     buf = torch.full((6, 511), 1.0, device="cuda").to(torch.float8_e4m3fn)
