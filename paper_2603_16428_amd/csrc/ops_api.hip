@@ -69,8 +69,13 @@ lce_status_t check_overlaps(std::initializer_list<std::pair<Rows, bool>> outs, s
 
 // ---- which threads share a row ----
 
-// As few threads as hold the row's values in up to four steps of 8 (a wave up to 1024 values, a quarter
-// of one for the rows of attention heads).
+// The threads that share a row, and their steps of 8 values. A wave or less needs no barrier, so up to 1024 values
+// are a wave's (32768 x 1024 in bf16, 128 threads against 64: forward 47.5 us against 47.3, backward 66.8 against
+// 65.9) or the part of one that they fill (131072 x 256: a whole wave, half of it idle, 51.8 and 78.9 us; 32 threads
+// 47.6 and 66.5); but no wave takes more steps instead of more threads, which few rows wait for (24 x 2048: 64
+// threads in four steps 3.1 and 6.2 us, 256 in one 2.5 and 4.7). Above, workgroups of 256 threads as long as four
+// steps do, then of 512 (4096 x 8192 in two steps of 512: 48.4 and 68.5 us against 49.0 and 69.2, e4m3 51.1 against
+// 49.7), of 1024 only where those do not hold the row (2730 x 12288: 51.8 and 77.5 us against 49.1 and 73.3).
 template <typename F>
 void by_width(int64_t H, F f) {
   auto go = [&](auto tpr, auto ch) { f(tpr, ch); };
@@ -78,6 +83,7 @@ void by_width(int64_t H, F f) {
 #define LCE_WIDTH(TPR, CH) \
   if (H <= (TPR) * (CH) * kNormVec) return go(integral_constant<int, TPR>{}, integral_constant<int, CH>{})
   LCE_WIDTH(16, 1);
+  LCE_WIDTH(32, 1);
   LCE_WIDTH(64, 1);
   LCE_WIDTH(64, 2);
   LCE_WIDTH(256, 1);
@@ -99,7 +105,8 @@ constexpr int64_t kForwardBlocks = int64_t(1) << 20;
 // Workgroups of the backward, each of which leaves H fp32 sums for dgamma: no more than keep the loads going.
 // One per CU where a thread holds 16 or more values of a row and those of the next one (8192 x 4096 in bf16:
 // 65 us, 68 with two, 76 with four), two where it holds 8 (16384 x 2048: 64 us, 70 with one; 262144 x 128: 42
-// and 58).
+// and 58). Of fewer rows than that each takes one, or two where the sums of one each would be 2 MB or more
+// (512 x 2048: 8.2 us against 10.2, 256 x 4096: 8.8 against 10.0; but 128 x 2048: 6.5 against 6.0).
 int64_t backward_blocks(int64_t N, int64_t H) {
   int64_t rows = 1, most = 256;
   by_width(H, [&](auto tpr, auto ch) {
@@ -107,7 +114,9 @@ int64_t backward_blocks(int64_t N, int64_t H) {
     rows = threads_of(kTpr) / kTpr;
     if (decltype(ch)::value == 1) most = 512;
   });
-  return std::max<int64_t>(1, std::min(cdiv(N, rows), most));
+  int64_t blocks = cdiv(N, rows);
+  if (blocks * H >= int64_t(1) << 19) blocks = cdiv(blocks, 2);
+  return std::max<int64_t>(1, std::min(blocks, most));
 }
 
 template <typename T, bool QUANT>

@@ -185,6 +185,9 @@ __device__ __forceinline__ void quantise(float (&s)[kNormVec], const RawRow<T>& 
   }
 }
 
+// TPR threads a row, several rows a workgroup where TPR is below 256. Bound by HBM: 8192 x 4096 in bf16 with a
+// residual 48 us (268 MB, 5.5 TB/s; a large copy moves 5.15), e4m3 in groups of 128 45 us (236 MB, 5.2 TB/s); one
+// row 2.6 us, the latency of a load and two barriers.
 template <typename T, int TPR, int CH, bool QUANT, RowEnd END>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(const NormArgs a) {
   constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR, kWaves = TPR > 64 ? TPR / 64 : 1;
@@ -279,7 +282,8 @@ struct NormBackwardArgs {
 //
 // Bound by HBM, so the loads may not stop while a row is reduced: AHEAD requests the next row's values
 // before the current one's dot product is joined. (A row's barrier and its joins take as long as its
-// loads.) What waits in registers waits in the input type.
+// loads.) What waits in registers waits in the input type. 8192 x 4096 in bf16, all of its tensors: 65 us
+// (336 MB, 5.1 TB/s; 106 in the first version, which held more in registers and requested less ahead).
 template <typename T, int TPR, int CH, RowEnd END, bool AHEAD>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_backward_kernel(const NormBackwardArgs a) {
   constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR, kWaves = TPR > 64 ? TPR / 64 : 1;

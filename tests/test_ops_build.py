@@ -41,9 +41,9 @@ def test_rows_are_in_registers(report):
         seen += 1
         backward, dtype, threads, steps = n
         assert use["ScratchSize"] == 0 or threads == 1024, (name, use)
-    # Ten widths, each with rows that end in whole and in part pieces, and the one for H < 8; three types; the
+    # Eleven widths, each with rows that end in whole and in part pieces, and the one for H < 8; three types; the
     # forward in its own type and in e4m3, and the backward.
-    assert seen == (2 * 10 + 1) * 3 * 3
+    assert seen == (2 * 11 + 1) * 3 * 3
 
 
 def test_gradient_kernels_are_resident_at_once(report):
