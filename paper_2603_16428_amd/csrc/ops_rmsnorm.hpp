@@ -5,8 +5,8 @@
 // bytes of a 16-bit type) of every 8 TPR, CH times. So every tensor is read and written once, whatever is
 // needed of the whole row (the mean square, the largest value, the backward's dot product) in between, and
 // an output may be an input's own memory: a row's values are all in registers before any is written. Loads
-// and stores are 16 bytes wide at any alignment of the element type; only the end of a row whose H is not
-// a multiple of 8 goes value by value.
+// and stores are 16 bytes wide at any alignment of the element type; only the last values of a row whose H is
+// not a multiple of 8 are stored one by one.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -330,8 +330,8 @@ def _check_grads(grads):
     strided, codes = torch.strided, DTYPES
     for g in grads:  # a model has hundreds: half a microsecond for each
         code = codes.get(g.dtype)
-        if code is None or g.layout is not strided:
-            raise ValueError("gradients must be dense bfloat16, float16 or float32 tensors")
+        if code is None or g.layout is not strided or g.is_neg():
+            raise ValueError("gradients must be dense bfloat16, float16 or float32 tensors, not lazily negated views")
         if g.get_device() != index:
             raise ValueError("gradients must be tensors of one device")
         if not (g.is_contiguous() or g.numel() == 0 or _dense(g)):
@@ -400,6 +400,6 @@ def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, out=None, wor
     else:
         out = [out] if isinstance(out, torch.Tensor) else [t for t in out if t is not None]
         if len(out) != len(grads) or any(t.shape != g.shape or t.dtype != g.dtype or t.device != dev
-                                         or (t.stride() != g.stride() and t.numel() > 1) for t, g in zip(out, grads)):
+                                         or (t.stride() != g.stride() and t.numel() > 1) or t.is_neg() for t, g in zip(out, grads)):
             raise ValueError("out must match the gradients in number, shape, strides, dtype and device")
     return _clip(grads, dev, table, max_norm, kind, out, workspace), out
