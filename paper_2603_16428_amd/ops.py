@@ -366,6 +366,8 @@ def grad_norm(grads, norm_type: float = 2.0, workspace: torch.Tensor | None = No
 
 
 def _clip(grads, dev, table, max_norm, norm_type, out, workspace):
+    if torch.nn.Parameter in map(type, grads):  # scaling the weights themselves is never meant
+        raise ValueError("clipping takes gradients, not parameters: [p.grad for p in parameters]")
     norm = grads[0].new_empty((), dtype=torch.float32)
     ws = _space(workspace, grads[0], grad_norm_workspace_size(len(grads)))
     outs = None if out is None else array.array("Q", [t.data_ptr() for t in out])

@@ -172,6 +172,7 @@ def test_versions_and_refusals(lce):
            lambda: lce.grad_norm([two[::2]]), lambda: lce.clip_grad_norm_([g, g.cpu()], 1.0), lambda: lce.grad_norm([g], 1.0),
            lambda: lce.clip_grad_norm([g], 1.0, out=[g[:32]]), lambda: lce.clip_grad_norm([g], 1.0, out=[]),
            lambda: lce.clip_grad_norm([two], 1.0, out=[two.clone().t().contiguous().t()]),
+           lambda: lce.clip_grad_norm_([torch.nn.Parameter(g)], 1.0), lambda: lce.clip_grad_norm([torch.nn.Parameter(g)], 1.0),
            lambda: lce.clip_grad_norm([torch._neg_view(g)], 1.0), lambda: lce.clip_grad_norm([g], 1.0, out=[torch._neg_view(g.clone())]),
            lambda: lce.clip_grad_norm([g], 1.0, out=[g.half()]), lambda: lce.grad_norm([g.to_sparse()])]
     for call in bad:
