@@ -110,7 +110,7 @@ def _check_rows(hidden, gamma):
     if not shape or shape[-1] < 1:
         raise ValueError("hidden must be [..., H]")
     H = shape[-1]
-    if gamma.shape != (H,) or gamma.dtype != dtype or gamma.device != dev:
+    if gamma.shape != (H,) or gamma.dtype is not dtype or gamma.get_device() != dev.index:
         raise ValueError("gamma must be [H] of the hidden dtype, on the hidden's device")
     if not gamma.is_contiguous() or gamma.is_neg() or hidden.is_neg():
         raise ValueError("gamma must be contiguous, and nothing a lazily negated view")
@@ -118,7 +118,7 @@ def _check_rows(hidden, gamma):
 
 
 def _check_like(t, shape, dtype, dev, what: str):
-    if t.shape != shape or t.dtype is not dtype or t.device != dev:
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev.index:
         raise ValueError(f"{what} must have the hidden's shape, dtype and device")
     if t.is_neg():
         raise ValueError(f"{what} is a lazily negated view: resolve_neg() it first")
@@ -133,38 +133,40 @@ def _written(tensors) -> None:
 
 
 def _output(t, like, dtype, what: str):
-    """A given output, checked, or a new one: rows of `like`'s shape."""
+    """A given output, checked, or a new one (rows of `like`'s shape), and its pitch."""
     if t is None:
-        return torch.empty_like(like, dtype=dtype) if like.is_contiguous() else like.new_empty(like.shape, dtype=dtype)
+        H = like.shape[-1]
+        if not like.is_contiguous():
+            return like.new_empty(like.shape, dtype=dtype), H
+        return torch.empty_like(like) if dtype is like.dtype else torch.empty_like(like, dtype=dtype), H
     _check_like(t, like.shape, dtype, like.device, what)
     _written([t])
-    return t
+    return t, _pitch(t, what)
 
 
 def _run_forward(hidden, residual, gamma, eps, quant, group_size, normed, added, return_rstd):
     N, H, shape, dtype, dev = _check_rows(hidden, gamma)
-    out = _output(normed, hidden, FP8 if quant else dtype, "normed")
+    out, out_pitch = _output(normed, hidden, FP8 if quant else dtype, "normed")
     scales = None
     if quant:
         scales = hidden.new_empty(shape[:-1] + (-(-H // group_size) if group_size else 1,), dtype=torch.float32)
     if residual is None:
         if added is not None:
             raise ValueError("without a residual there is no sum: it is hidden itself")
-        total = hidden
+        total, res, res_pitch, total_ptr, total_pitch = hidden, None, 0, None, 0
     else:
         _check_like(residual, shape, dtype, dev, "residual")
-        total = _output(added, hidden, dtype, "added")
+        total, total_pitch = _output(added, hidden, dtype, "added")
+        res, res_pitch, total_ptr = residual.data_ptr(), _pitch(residual, "residual"), total.data_ptr()
     rstd = hidden.new_empty(shape[:-1], dtype=torch.float32) if return_rstd else None
     if N:
-        rows = (hidden.data_ptr(), _pitch(hidden, "hidden"), *_optional(residual, "residual"), gamma.data_ptr(), N, H,
-                DTYPES[dtype], eps)
-        sums = _optional(None if residual is None else total, "added")
         r = None if rstd is None else rstd.data_ptr()
         if quant:
-            _call("lce_add_rmsnorm_quant", dev, *rows, group_size, out.data_ptr(), _pitch(out, "normed"),
-                  scales.data_ptr(), *sums, r)
+            _call("lce_add_rmsnorm_quant", dev, hidden.data_ptr(), _pitch(hidden, "hidden"), res, res_pitch, gamma.data_ptr(),
+                  N, H, DTYPES[dtype], eps, group_size, out.data_ptr(), out_pitch, scales.data_ptr(), total_ptr, total_pitch, r)
         else:
-            _call("lce_add_rmsnorm_forward", dev, *rows, out.data_ptr(), _pitch(out, "normed"), *sums, r)
+            _call("lce_add_rmsnorm_forward", dev, hidden.data_ptr(), _pitch(hidden, "hidden"), res, res_pitch, gamma.data_ptr(),
+                  N, H, DTYPES[dtype], eps, out.data_ptr(), out_pitch, total_ptr, total_pitch, r)
     outs = (out, scales, total) if quant else (out, total)
     return outs + (rstd,) if return_rstd else outs
 
@@ -216,7 +218,7 @@ def add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd,
         _check_like(residual, shape, dtype, dev, "residual")
     if rstd.shape != shape[:-1] or rstd.dtype != torch.float32 or rstd.device != dev or not rstd.is_contiguous():
         raise ValueError("rstd must be the forward call's")
-    dx = _output(grad_hidden, hidden, dtype, "grad_hidden")
+    dx, dx_pitch = _output(grad_hidden, hidden, dtype, "grad_hidden")
     dg = ws = None
     size = 0
     if need_gamma:
@@ -231,7 +233,7 @@ def add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd,
     _call("lce_add_rmsnorm_backward", dev, grad_normed.data_ptr(), _pitch(grad_normed, "grad_normed"),
           *_optional(grad_added, "grad_added"), hidden.data_ptr(), _pitch(hidden, "hidden"),
           *_optional(residual, "residual"), gamma.data_ptr(), rstd.data_ptr(), N, H, DTYPES[dtype],
-          dx.data_ptr(), _pitch(dx, "grad_hidden"), None if dg is None else dg.data_ptr(),
+          dx.data_ptr(), dx_pitch, None if dg is None else dg.data_ptr(),
           None if ws is None else ws.data_ptr(), size)
     return dx, dg
 
