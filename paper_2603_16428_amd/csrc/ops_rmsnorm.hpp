@@ -153,11 +153,23 @@ constexpr float kScaleMin = 1.17549435e-38f;  // 2^-126
 // value. What is left is the rounding of top and of the result: half as many values as in plain fp32 lie on the
 // other side of a border than in 64 bits. (In 64-bit products none do, but 8192 x 4096 in bf16 take
 // 48.5 us; 45.4 so, and 43.7 in plain fp32.)
+//
+// s comes here times r's power of two, and r without it, in [1, 2): u is then at most normed and more than half of
+// it, so it leaves fp32 only where normed does. Without that, s gamma of a row of small values may be 2^8 times
+// smaller than normed, and 448 / top infinite beside an ordinary scale. (One product a value: 0.7 us of 40.)
+struct RowScale {
+  float p, r;  // 1 / rms = p r; p a power of two
+};
+__device__ __forceinline__ RowScale row_scale(float r) {
+  // (r = 0 where a value or the mean square is infinite: finite values become 0 at once. A NaN stays one.)
+  return {r == 0.f ? 0.f : __builtin_amdgcn_ldexpf(1.f, __builtin_amdgcn_frexp_expf(r) - 1), 2.f * __builtin_amdgcn_frexp_mantf(r)};
+}
 struct QuantFactor {
   float inv, inv_lo, r;
-  bool tiny;  // the scale is at its least: all values are far below 2^-126
+  bool tiny;  // the scale is at its least: no value is above 448 x 2^-126
 };
-// From the largest |u| of a group, by its bits (among which a NaN's are above all others).
+// From the largest |u| of a group, by its bits (among which a NaN's are above all others). Where the scale is not
+// at its least, top is above 448 x 2^-127 and 448 / top at most 2^127.
 __device__ __forceinline__ QuantFactor quant_factor(uint32_t top_bits, float r, float& scale) {
   const float top = __builtin_bit_cast(float, top_bits);
   const float sc = top * (r * (1.f / kFp8Max));
@@ -226,6 +238,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
     const float r = rsqrtf(fmaf(ss, inv_h, a.eps));
     if (live && t == 0 && a.rstd != nullptr) a.rstd[i] = r;
     uint32_t top = 0;
+    const RowScale rs = QUANT ? row_scale(r) : RowScale{};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       const int c = (k * TPR + t) * kNormVec, n = live ? a.H - c : 0;
@@ -237,13 +250,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
       } else {
         uint32_t m = 0;
 #pragma unroll
+        for (int e = 0; e < kNormVec; ++e) s[k][e] *= rs.p;
+#pragma unroll
         for (int e = 0; e < kNormVec; ++e) m = MaxOp::of(m, __builtin_bit_cast(uint32_t, s[k][e] * gamma[k].at(e)) & 0x7fffffffu);
         if (a.group == 0) {
           top = MaxOp::of(top, m);
         } else {
           for (int o = 1; o < a.group / kNormVec; o <<= 1) m = MaxOp::of(m, (uint32_t)__shfl_xor((int)m, o));
           float scale;
-          const QuantFactor f = quant_factor(m, r, scale);
+          const QuantFactor f = quant_factor(m, rs.r, scale);
           if (n > 0 && c % a.group == 0) a.scales[i * ((a.H + a.group - 1) / a.group) + c / a.group] = scale;
           quantise(s[k], gamma[k], f);
           store_row_fp8<END>((uint8_t*)a.normed + i * a.normed_ld + c, n, s[k]);
@@ -254,7 +269,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void add_rmsnorm_kernel(cons
       if (a.group == 0) {
         top = row_reduce<TPR, MaxOp>(top, tops[turn]);
         float scale;
-        const QuantFactor f = quant_factor(top, r, scale);
+        const QuantFactor f = quant_factor(top, rs.r, scale);
         if (live && t == 0) a.scales[i] = scale;
 #pragma unroll
         for (int k = 0; k < CH; ++k) {

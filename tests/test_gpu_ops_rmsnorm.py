@@ -228,6 +228,50 @@ def test_quant_at_the_smallest_scale(lce):
             assert q.float().abs().max() > 0.1
 
 
+def _check_quant(lce, x, res, gamma, group, eps=EPS):
+    """test_quant's bounds, and 8 of fp32's own smallest steps for values next to the smallest scale."""
+    q, scales, added = lce.add_rmsnorm_quant(x, res, gamma, eps, group)
+    N, H = x.shape
+    y, _, _ = O.add_rmsnorm(x, res, gamma, eps)
+    want = O.group_scales(y, group)
+    _near(scales.view(N, -1), want, 36 * W)
+    wide = want.repeat_interleave(group or H, 1)[:, :H]
+    values = q.float().cpu().double() * scales.view(N, -1).cpu().double().repeat_interleave(group or H, 1)[:, :H]
+    bound = torch.maximum(2.0 ** -4 * y.abs(), 2.0 ** -10 * wide) + 96 * W * y.abs() + 8 * 2.0 ** -149
+    assert bool(((values - y).abs() <= bound).all())  # false where a value is NaN
+    top = torch.nn.functional.pad(q.float().cpu().abs(), (0, -H % (group or H))).view(N, -1, group or H).amax(-1)
+    assert bool((top[want > O.SCALE_MIN * (1 + 36 * W)] == 448).all())
+
+
+@pytest.mark.parametrize("group", [0, 32, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("H", [6, 264, 4096])
+def test_quant_of_tiny_groups(lce, H, dtype, group):
+    """Finite scales around the least one, in rows of every size: gains that have decayed to almost nothing,
+    throughout a row and in one group beside ordinary ones; rows of such values."""
+    g = torch.Generator().manual_seed(H + group)
+    rms = torch.tensor([1.0, 0.2, 0.02, 0.002]).repeat_interleave(3)[:, None]
+    x, res = ((rms * torch.randn((12, H), generator=g) / 2 ** 0.5).to(DT[dtype]).cuda() for _ in range(2))
+    gain = 1.0 + 0.2 * torch.randn(H, generator=g)
+    for e in range(-132, -100, 2):
+        _check_quant(lce, x, res, (gain * 2.0 ** e).to(DT[dtype]).cuda(), group)
+        one = gain.clone()
+        one[32:64] *= 2.0 ** e
+        _check_quant(lce, x, res, one.to(DT[dtype]).cuda(), group)
+    sizes = torch.tensor([2e-36, 1e-36, 5e-37, 1e-37, 1e-38, 1e-40])[:, None]
+    rows = [(sizes * torch.randn((6, H), generator=g)).to(DT[dtype]).cuda() for _ in range(2)]
+    _check_quant(lce, *rows, gain.to(DT[dtype]).cuda(), group)
+    _check_quant(lce, rows[0], None, gain.to(DT[dtype]).cuda(), group)
+
+
+def test_quant_of_any_product(lce):
+    """Rows and gains whose products leave fp32 while the normalised values do not."""
+    x, res, gamma, _, _ = _inputs(9, 257, "fp32")
+    for size, gain in ((1e15, 1e28), (1e15, 1e-35), (1e-15, 1e-30), (1e-15, 1e35)):
+        for group in (0, 32):
+            _check_quant(lce, x * size, res * size, gamma * gain, group, eps=0.0)
+
+
 def test_quant_into_a_wider_buffer(lce):
     x, r, gamma, _, _ = _inputs(6, 300, "bf16")
     buf = torch.full((6, 511), 1.0, device="cuda").to(torch.float8_e4m3fn)
