@@ -110,6 +110,8 @@ lce_status_t lce_add_rmsnorm_backward(const void* grad_normed, int64_t grad_norm
  *   norm      : device fp32 [1].
  *   workspace : device memory of lce_grad_norm_workspace_size(count) bytes, 256-byte aligned. Calls
  *               (and captured graphs) that may run at the same time need one each.
+ * norm and workspace overlap no tensor of the call and not each other, else LCE_ERR_INVALID_ARGUMENT;
+ * gradients that are only read (lce_grad_norm) may overlap.
  * All the values together are below 2^31 pieces of 16 KB.
  */
 typedef struct {

@@ -167,6 +167,19 @@ int64_t count_pieces(const lce_tensor_t* grads, int64_t count, std::vector<Tenso
   return pieces;
 }
 
+// Whether the norm or the workspace, which every call writes, overlap each other or a gradient.
+bool norm_overlaps(const std::vector<TensorEntry>& table, const float* norm, const void* workspace) {
+  const int64_t space = (int64_t)lce_grad_norm_workspace_size((int64_t)table.size());
+  const Rows n{norm, sizeof(float), sizeof(float), 1}, w{workspace, space, space, 1};
+  if (overlap(n, w)) return true;
+  for (const TensorEntry& e : table) {
+    const int64_t bytes = e.n * size_of(e.dtype);
+    const Rows g{bytes > 0 ? e.in : nullptr, bytes, bytes, 1};
+    if (overlap(g, n) || overlap(g, w)) return true;
+  }
+  return false;
+}
+
 // Whether memory that a clip writes (the norm and the workspace too) overlaps any other of the call; out[k] may
 // be grads[k].data.
 bool clip_overlaps(const std::vector<TensorEntry>& table, const float* norm, const void* workspace) {
@@ -261,7 +274,7 @@ lce_status_t grad_norm_call(const lce_tensor_t* grads, int64_t count, int norm_t
     const int64_t pieces = count_pieces(grads, count, table, out);
     if (pieces < 0) return LCE_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < lce_grad_norm_workspace_size(count)) return LCE_ERR_WORKSPACE_TOO_SMALL;
-    if ((uintptr_t)workspace % 256 != 0 || (clip && clip_overlaps(table, norm, workspace))) return LCE_ERR_INVALID_ARGUMENT;
+    if ((uintptr_t)workspace % 256 != 0 || (clip ? clip_overlaps : norm_overlaps)(table, norm, workspace)) return LCE_ERR_INVALID_ARGUMENT;
     return norm_type == LCE_NORM_INF ? run_norm<true>(table, pieces, clip, out == nullptr, max_norm, norm, workspace, s)
                                      : run_norm<false>(table, pieces, clip, out == nullptr, max_norm, norm, workspace, s);
   } catch (...) {

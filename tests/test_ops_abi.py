@@ -155,6 +155,17 @@ def test_grad_norm_validation(lib):
     assert 0 < sizes[0] == sizes[1] < sizes[2] < sizes[3]
 
 
+@pytest.mark.parametrize("count", [1, 200])
+def test_grad_norm_writes_no_gradient(lib, count):
+    """The norm and the workspace (its table of more than 112 gradients too) overlap neither a gradient nor each other.
+    (Gradients that are only read may overlap: the GPU tests read one twice.)"""
+    need = lib.lce_grad_norm_workspace_size(count)
+    grads = [(X + 4096 * k, 100, BF16) for k in range(count - 1)] + [(R, 1 << 20, FP32)]
+    for entries in (grads, grads[::-1]):
+        for norm, ws in ((R, WS), (R + (4 << 20) - 4, WS), (SC, R), (SC, R + (4 << 20) - 256), (SC, R - need + 256), (WS, WS), (WS + need - 4, WS)):
+            assert lib.lce_grad_norm(_list(*entries), count, 0, norm, ws, 1 << 20, None) == INVALID
+
+
 def test_binding_refuses():
     import torch
     import paper_2603_16428_amd as lce
