@@ -82,6 +82,7 @@ lce_status_t lce_add_rmsnorm_quant(const void* x, int64_t x_ld, const void* resi
  *   grad_gamma  : device [H] of dtype, summed over the rows in fp32 in a fixed order; NULL where it is
  *                 not wanted (no workspace then). N = 0 gives zeros.
  *   workspace   : device memory of lce_add_rmsnorm_workspace_size(N, H, dtype) bytes, 256-byte aligned.
+ *                 The size does not fall as N grows: one for the largest batch serves the smaller ones.
  */
 size_t lce_add_rmsnorm_workspace_size(int64_t N, int64_t H, int dtype);
 lce_status_t lce_add_rmsnorm_backward(const void* grad_normed, int64_t grad_normed_ld, const void* grad_added,

@@ -107,16 +107,30 @@ constexpr int64_t kForwardBlocks = int64_t(1) << 20;
 // 65 us, 68 with two, 76 with four), two where it holds 8 (16384 x 2048: 64 us, 70 with one; 262144 x 128: 42
 // and 58). Of fewer rows than that each takes one, or two where the sums of one each would be 2 MB or more
 // (512 x 2048: 8.2 us against 10.2, 256 x 4096: 8.8 against 10.0; but 128 x 2048: 6.5 against 6.0).
-int64_t backward_blocks(int64_t N, int64_t H) {
-  int64_t rows = 1, most = 256;
+constexpr int64_t kGammaSums = int64_t(1) << 19;
+struct BackwardGrid {
+  int64_t rows, most;  // rows a workgroup takes at a time; workgroups at most
+};
+BackwardGrid backward_grid(int64_t H) {
+  BackwardGrid g{1, 256};
   by_width(H, [&](auto tpr, auto ch) {
     constexpr int kTpr = decltype(tpr)::value;
-    rows = threads_of(kTpr) / kTpr;
-    if (decltype(ch)::value == 1) most = 512;
+    g.rows = threads_of(kTpr) / kTpr;
+    if (decltype(ch)::value == 1) g.most = 512;
   });
-  int64_t blocks = cdiv(N, rows);
-  if (blocks * H >= int64_t(1) << 19) blocks = cdiv(blocks, 2);
-  return std::max<int64_t>(1, std::min(blocks, most));
+  return g;
+}
+int64_t backward_blocks(int64_t N, int64_t H) {
+  const BackwardGrid g = backward_grid(H);
+  int64_t blocks = cdiv(N, g.rows);
+  if (blocks * H >= kGammaSums) blocks = cdiv(blocks, 2);
+  return std::max<int64_t>(1, std::min(blocks, g.most));
+}
+// The most workgroups that N rows or fewer take: the last number of rows before two a workgroup may take more than N.
+// (So a workspace for N rows serves any smaller batch.)
+int64_t workspace_blocks(int64_t N, int64_t H) {
+  const int64_t one_each = (kGammaSums - 1) / H * backward_grid(H).rows;
+  return std::max(backward_blocks(N, H), backward_blocks(std::min(N, one_each), H));
 }
 
 template <typename T, bool QUANT>
@@ -347,7 +361,7 @@ lce_status_t lce_add_rmsnorm_quant(const void* x, int64_t x_ld, const void* resi
 
 size_t lce_add_rmsnorm_workspace_size(int64_t N, int64_t H, int dtype) {
   if (lce::check_rows(N, H, dtype) != LCE_OK) return 0;
-  return (size_t)lce::cdiv(lce::backward_blocks(N, H) * H * 4, 256) * 256;
+  return (size_t)lce::cdiv(lce::workspace_blocks(N, H) * H * 4, 256) * 256;
 }
 
 lce_status_t lce_add_rmsnorm_backward(const void* grad_normed, int64_t grad_normed_ld, const void* grad_added,

@@ -102,6 +102,16 @@ def test_backward_workspace(lib):
     assert f(1 << 30, 32768, FP32) <= 1024 * 32768 * 4
 
 
+@pytest.mark.parametrize("H", [5, 64, 128, 200, 256, 500, 512, 768, 1000, 1024, 2048, 4096, 6000, 8192, 12288, 16384, 20000, 32768])
+def test_backward_workspace_of_a_batch_serves_smaller_ones(lib, H):
+    size = lib.lce_add_rmsnorm_workspace_size
+    sizes = [size(N, H, BF16) for N in [*range(5000), *range(5000, 300000, 997), 1 << 30]]
+    assert sizes == sorted(sizes)
+    # And the call takes it (up to the check behind the size's: an unaligned workspace).
+    for N in (1, 15, 100, 127, 128, 255):
+        assert _backward(lib, N=N, H=H, dtype=BF16, wsb=size(256, H, BF16), ws=WS + 64, **{k: H for k in ("dy_ld", "ds_ld", "x_ld", "r_ld", "dx_ld")}) == INVALID
+
+
 class Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
