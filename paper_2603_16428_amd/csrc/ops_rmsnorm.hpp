@@ -113,7 +113,9 @@ __device__ __forceinline__ void store_row_fp8(uint8_t* p, int n, const float (&v
 }
 
 // The TPR threads' sum (or, of bit patterns, maximum) of a row, in a fixed order, for all of them. More
-// than a wave's goes through `lds`, one entry per wave; two buffers in turn need one barrier a row.
+// than a wave's goes through `lds`, one entry per wave; two buffers in turn need one barrier a row. More than four
+// waves' are joined in pairs: a chain of 16 would round more often than all that is before it, a thread's 32 terms
+// apart. So no value goes through more than 10 joins.
 struct AddOp {
   static __device__ __forceinline__ float of(float a, float b) { return a + b; }
 };
@@ -127,9 +129,21 @@ __device__ __forceinline__ V row_reduce(V v, V* lds) {
   if constexpr (TPR > 64) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = lds[0];
+    constexpr int kWaves = TPR / 64;
+    if constexpr (kWaves > 4) {
+      V of[kWaves];
 #pragma unroll
-    for (int w = 1; w < TPR / 64; ++w) v = Op::of(v, lds[w]);
+      for (int w = 0; w < kWaves; ++w) of[w] = lds[w];
+#pragma unroll
+      for (int n = kWaves / 2; n > 0; n /= 2)
+#pragma unroll
+        for (int w = 0; w < n; ++w) of[w] = Op::of(of[w], of[w + n]);
+      v = of[0];
+    } else {
+      v = lds[0];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) v = Op::of(v, lds[w]);
+    }
   }
   return v;
 }

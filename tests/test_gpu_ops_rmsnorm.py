@@ -186,6 +186,19 @@ def test_eps_zero_and_tiny_values(lce):
         _check_forward(*lce.add_rmsnorm_forward(x * scale, r * scale, gamma, 0.0), None, x * scale, r * scale, gamma, 0.0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_sums_of_many_waves(lce, dtype):
+    """The 16 waves of the widest rows hold 2^24 and fifteen ones (their squares are exact). Joined in pairs, four
+    roundings of w at most: 2 w in r, and 2 w for the rsqrt. Joined in a chain every one is lost: 15 w, 7.5 w in r."""
+    x = torch.zeros((3, 32768), dtype=DT[dtype], device="cuda")
+    x[:, ::512][:, :16] = 1.0
+    x[:, 0] = 4096.0
+    gamma = torch.ones(32768, dtype=DT[dtype], device="cuda")
+    _, _, r = lce.add_rmsnorm_forward(x, None, gamma, 0.0, return_rstd=True)
+    want = ((2.0 ** 24 + 15) / 32768) ** -0.5
+    assert bool(((r.cpu().double() - want).abs() <= 4 * W * want).all())
+
+
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("group", [0, 32, 64, 128])
 @pytest.mark.parametrize("H", [1, 8, 31, 33, 100, 128, 129, 136, 250, 256, 512, 520, 1024, 1030, 2048, 4096, 4100, 6000, 8192, 12288, 16384, 20000])
