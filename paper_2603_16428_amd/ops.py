@@ -12,7 +12,7 @@ import ctypes
 
 import torch
 
-from .lce import DTYPES, LCE_OK, LCEError, _bytes_are_values, load_library
+from .lce import DTYPES, LCE_OK, LCEError, _bytes_are_values, _differentiated, load_library
 
 EXPORTED = ("lce_add_rmsnorm_forward", "lce_add_rmsnorm_quant", "lce_add_rmsnorm_workspace_size",
             "lce_add_rmsnorm_backward", "lce_grad_norm_workspace_size", "lce_grad_norm", "lce_clip_grad_norm")
@@ -178,8 +178,8 @@ def add_rmsnorm_forward(hidden, residual, gamma, eps: float = 1e-5, normed=None,
     hidden [..., H] and residual (or None: added is hidden itself) need consecutive values in a row and
     evenly spaced rows, not contiguity. The sum is normalised in fp32, before its rounding. `normed` and
     `added` may be given, and may be hidden or residual themselves (a residual stream updated in place).
-    rstd [...] (fp32) is 1 / sqrt(mean(added^2) + eps), for add_rmsnorm_backward. Not differentiable: see
-    add_rmsnorm.
+    rstd [...] (fp32) is 1 / sqrt(mean(added^2) + eps), for add_rmsnorm_backward. Not differentiable, in
+    forward mode either: see add_rmsnorm.
     """
     return _run_forward(hidden, residual, gamma, eps, False, 0, normed, added, return_rstd)
 
@@ -190,7 +190,7 @@ def add_rmsnorm_quant(hidden, residual, gamma, eps: float = 1e-5, group_size: in
 
     Each group of `group_size` (32, 64 or 128; 0: the whole row) consecutive values of a row has one fp32
     scale, its largest magnitude / 448: quantised * scale stands for the value. scales is
-    [..., ceil(H / group_size)] ([..., 1] with a scale per row).
+    [..., ceil(H / group_size)] ([..., 1] with a scale per row). Not differentiable.
     """
     if group_size not in GROUP_SIZES:
         raise ValueError(f"group_size must be one of {GROUP_SIZES}")
@@ -342,6 +342,22 @@ def _check_grads(grads):
     return grads, grads[0].device, array.array("q", flat)
 
 
+class _Undifferentiated(torch.autograd.Function):
+    """What a call gives for tensors that autograd follows: differentiating it raises, instead of finding constants."""
+
+    @staticmethod
+    def forward(ctx, call, *followed):
+        return call()
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the gradients' norm and clipping are not differentiable: detach() them to use them as constants")
+
+    @staticmethod
+    def jvp(ctx, *tangents):
+        _Undifferentiated.backward(ctx)
+
+
 def _norm_type(norm_type):
     if norm_type not in NORM_TYPES:
         raise ValueError("norm_type must be 2.0 or inf")
@@ -357,14 +373,19 @@ def grad_norm(grads, norm_type: float = 2.0, workspace: torch.Tensor | None = No
     """The norm (2 or inf) over all values of the gradients: a device scalar in fp32, squares summed in fp64.
 
     grads: device tensors (Nones among them are left out) of one device and any of the three types, each
-    filling one block of memory.
+    filling one block of memory. Not differentiable: of gradients with a graph of their own (create_graph) the
+    norm raises if it is differentiated.
     """
     kind = _norm_type(norm_type)
     grads, dev, table = _check_grads(grads)
-    norm = grads[0].new_empty((), dtype=torch.float32)
-    ws = _space(workspace, grads[0], grad_norm_workspace_size(len(grads)))
-    _call("lce_grad_norm", dev, table.buffer_info()[0], len(grads), kind, norm.data_ptr(), ws.data_ptr(), ws.numel())
-    return norm
+
+    def call():
+        norm = grads[0].new_empty((), dtype=torch.float32)
+        ws = _space(workspace, grads[0], grad_norm_workspace_size(len(grads)))
+        _call("lce_grad_norm", dev, table.buffer_info()[0], len(grads), kind, norm.data_ptr(), ws.data_ptr(), ws.numel())
+        return norm
+
+    return _Undifferentiated.apply(call, *grads) if _differentiated(grads) else call()
 
 
 def _clip(grads, dev, table, max_norm, norm_type, out, workspace):
@@ -385,6 +406,8 @@ def clip_grad_norm_(grads, max_norm: float, norm_type: float = 2.0, workspace: t
 
     The factor is min(1, max_norm / (norm + 1e-6)). Nothing waits for the norm: it and the factor stay on
     the device, and gradients within the limit are not written. A NaN among the gradients makes all NaN.
+    Autograd does not see it, as if under torch.no_grad(): the norm is a constant, and gradients with a graph
+    of their own keep the one they had.
     """
     kind = _norm_type(norm_type)
     grads, dev, table = _check_grads(grads)
@@ -395,15 +418,21 @@ def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, out=None, wor
     """(norm, clipped): as clip_grad_norm_, with the scaled gradients in other memory.
 
     out: tensors of the gradients' shapes, strides and types (for instance those that a copy to the host
-    reads), one for each gradient that is not None; new ones by default.
+    reads), one for each gradient that is not None; new ones by default. Not differentiable: of gradients
+    with a graph of their own the norm and new tensors raise if they are differentiated.
     """
     kind = _norm_type(norm_type)
     grads, dev, table = _check_grads(grads)
-    if out is None:
-        out = [torch.empty_like(g) for g in grads]
-    else:
+    if out is not None:
         out = [out] if isinstance(out, torch.Tensor) else [t for t in out if t is not None]
         if len(out) != len(grads) or any(t.shape != g.shape or t.dtype != g.dtype or t.device != dev
                                          or (t.stride() != g.stride() and t.numel() > 1) or t.is_neg() for t, g in zip(out, grads)):
             raise ValueError("out must match the gradients in number, shape, strides, dtype and device")
-    return _clip(grads, dev, table, max_norm, kind, out, workspace), out
+
+    def call():
+        outs = [torch.empty_like(g) for g in grads] if out is None else out
+        norm = _clip(grads, dev, table, max_norm, kind, outs, workspace)
+        return (norm, *outs) if out is None else (norm,)
+
+    norm, *new = _Undifferentiated.apply(call, *grads) if _differentiated(grads) else call()
+    return norm, new if out is None else out

@@ -190,6 +190,36 @@ def test_versions_and_refusals(lce):
     assert float(lce.grad_norm([g, g])) == pytest.approx(math.sqrt(128), rel=W)  # reading twice is fine
 
 
+def test_gradients_with_a_graph(lce):
+    """Gradients made under create_graph: the values are as ever, and differentiating them raises."""
+    x = torch.linspace(-1.0, 2.0, 500, device="cuda").requires_grad_()
+    y = torch.linspace(1.0, 3.0, 300, device="cuda")
+    g, = torch.autograd.grad((x ** 3).sum(), x, create_graph=True)
+    want, clipped = O.clip([g, y], 2.0)
+    for norm, outs in [(lce.grad_norm([g, y]), None), lce.clip_grad_norm([g, y], 2.0),
+                       lce.clip_grad_norm([y, g], 2.0, out=[y.new_empty(300), y.new_empty(500)])]:
+        assert abs(float(norm.detach()) - float(want)) <= (W * 1.001 + 1e-12) * float(want)
+        for t in (norm, *(outs or ())):
+            if t.requires_grad:
+                with pytest.raises(RuntimeError):
+                    torch.autograd.grad((t * t).sum() + (g * g).sum(), x, retain_graph=True)
+        assert norm.requires_grad
+    norm, outs = lce.clip_grad_norm([g, y], 2.0)
+    _check(norm.detach(), [t.detach() for t in outs], [g.detach(), y], 2.0)
+    assert outs[0].requires_grad and outs[1].requires_grad
+    with torch.no_grad():
+        assert not lce.grad_norm([g, y]).requires_grad
+    norm = lce.clip_grad_norm_([g, y], 2.0)
+    assert not norm.requires_grad and torch.equal(g.detach(), outs[0].detach()) and g.requires_grad
+    # Nothing to follow: constants.
+    norm, outs = lce.clip_grad_norm([y], 2.0)
+    assert not norm.requires_grad and not outs[0].requires_grad and isinstance(outs, list)
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(y, torch.ones_like(y))
+        with pytest.raises(RuntimeError):
+            lce.grad_norm([dual])
+
+
 @pytest.mark.parametrize("count", [20, 130])
 def test_streams_and_graphs(lce, count):
     """Clipping captured with few tensors (in the launch's arguments) and with many (their table in the workspace),
