@@ -389,7 +389,7 @@ def grad_norm(grads, norm_type: float = 2.0, workspace: torch.Tensor | None = No
 
 
 def _clip(grads, dev, table, max_norm, norm_type, out, workspace):
-    if torch.nn.Parameter in map(type, grads):  # scaling the weights themselves is never meant
+    if any(issubclass(c, torch.nn.Parameter) for c in set(map(type, grads))):  # scaling the weights themselves is never meant
         raise ValueError("clipping takes gradients, not parameters: [p.grad for p in parameters]")
     norm = grads[0].new_empty((), dtype=torch.float32)
     ws = _space(workspace, grads[0], grad_norm_workspace_size(len(grads)))
@@ -411,6 +411,8 @@ def clip_grad_norm_(grads, max_norm: float, norm_type: float = 2.0, workspace: t
     """
     kind = _norm_type(norm_type)
     grads, dev, table = _check_grads(grads)
+    if any([g.is_leaf for g in grads if g.requires_grad]):
+        raise ValueError("a leaf that requires a gradient is a weight, not a gradient: [p.grad for p in parameters]")
     return _clip(grads, dev, table, max_norm, kind, None, workspace)
 
 

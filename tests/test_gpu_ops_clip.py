@@ -220,6 +220,30 @@ def test_gradients_with_a_graph(lce):
             lce.grad_norm([dual])
 
 
+def test_weights_are_not_scaled(lce):
+    """Leaves that require a gradient, and parameters of any class, frozen ones too: refused, and left as they were."""
+    class Weight(torch.nn.Parameter):
+        pass
+
+    w = torch.ones(64, device="cuda")
+    leaf = w.clone().requires_grad_()
+    for bad in (leaf, Weight(w.clone()), Weight(w.clone(), requires_grad=False), torch.nn.Parameter(w.clone(), requires_grad=False)):
+        for call in (lambda: lce.clip_grad_norm_([w.clone(), bad], 1.0), lambda: lce.clip_grad_norm_(bad, 1.0)):
+            with pytest.raises(ValueError):
+                call()
+        with torch.no_grad(), pytest.raises(ValueError):
+            lce.clip_grad_norm_([bad], 1.0)
+        assert torch.equal(bad.detach(), w)
+    with pytest.raises(ValueError):
+        lce.clip_grad_norm([Weight(w)], 1.0)
+    # What a leaf's backward leaves in .grad is clipped, also where it has a graph.
+    (leaf ** 2).sum().backward()
+    assert float(lce.clip_grad_norm_([leaf.grad], 1.0)) == 16.0 and float(lce.grad_norm(leaf.grad)) == pytest.approx(1.0, abs=1e-6)
+    leaf.grad = torch.autograd.grad((leaf ** 2).sum(), leaf, create_graph=True)[0]
+    # 2 / (16 + 1e-6), one w below 0.125: the factor's rounding, the product's and the 1e-6 are 3 w together.
+    assert float(lce.clip_grad_norm_([leaf.grad], 1.0)) == 16.0 and abs(float(leaf.grad[0].detach()) - 2 / (16 + 1e-6)) <= 3 * W * 0.125
+
+
 @pytest.mark.parametrize("count", [20, 130])
 def test_streams_and_graphs(lce, count):
     """Clipping captured with few tensors (in the launch's arguments) and with many (their table in the workspace),
