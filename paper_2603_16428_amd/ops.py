@@ -132,6 +132,12 @@ def _written(tensors) -> None:
         torch.autograd.graph.increment_version([t for t in tensors if not t.is_inference()])
 
 
+def _check_unfollowed(t, what: str) -> None:
+    """A given output must not have a graph: it would keep it, and say that it is something else."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what} requires a gradient, and this call is not differentiable: give it detached, or call under torch.no_grad()")
+
+
 def _output(t, like, dtype, what: str):
     """A given output, checked, or a new one (rows of `like`'s shape), and its pitch."""
     if t is None:
@@ -140,6 +146,7 @@ def _output(t, like, dtype, what: str):
             return like.new_empty(like.shape, dtype=dtype), H
         return torch.empty_like(like) if dtype is like.dtype else torch.empty_like(like, dtype=dtype), H
     _check_like(t, like.shape, dtype, like.device, what)
+    _check_unfollowed(t, what)
     _written([t])
     return t, _pitch(t, what)
 
@@ -178,6 +185,7 @@ def add_rmsnorm_forward(hidden, residual, gamma, eps: float = 1e-5, normed=None,
     hidden [..., H] and residual (or None: added is hidden itself) need consecutive values in a row and
     evenly spaced rows, not contiguity. The sum is normalised in fp32, before its rounding. `normed` and
     `added` may be given, and may be hidden or residual themselves (a residual stream updated in place).
+    Given outputs, here and in the calls below, must not require a gradient where gradients are recorded.
     rstd [...] (fp32) is 1 / sqrt(mean(added^2) + eps), for add_rmsnorm_backward. Not differentiable, in
     forward mode either: see add_rmsnorm.
     """
@@ -430,6 +438,8 @@ def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, out=None, wor
         if len(out) != len(grads) or any(t.shape != g.shape or t.dtype != g.dtype or t.device != dev
                                          or (t.stride() != g.stride() and t.numel() > 1) or t.is_neg() for t, g in zip(out, grads)):
             raise ValueError("out must match the gradients in number, shape, strides, dtype and device")
+        for t in out:
+            _check_unfollowed(t, "out")
 
     def call():
         outs = [torch.empty_like(g) for g in grads] if out is None else out

@@ -94,3 +94,26 @@ def test_evaluation_in_eight_bits(lce):
     y, _, _ = O.add_rmsnorm(d["hidden"], res, gamma, EPS)
     got = rows.cpu().double().numpy()
     assert np.abs(got - y.numpy()).max() <= (2.0 ** -4 + 2.0 ** -8) * np.abs(y.numpy()).max()
+
+
+def test_outputs_that_autograd_follows(lce):
+    """A given output with a graph of its own would say that it is still what that graph computed: refused where
+    gradients are recorded, and fine without."""
+    x, r, dy = (torch.linspace(-1.0, 2.0, 256, device="cuda").view(4, 64) * k for k in (1.0, 2.0, 3.0))
+    gamma, rstd = torch.ones(64, device="cuda"), torch.ones(4, device="cuda")
+    leaf = x.clone().requires_grad_()
+
+    def followed():
+        return leaf * 1.0
+
+    for call in (lambda t: lce.add_rmsnorm_forward(x, r, gamma, EPS, normed=t), lambda t: lce.add_rmsnorm_forward(t, r, gamma, EPS, added=t),
+                 lambda t: lce.add_rmsnorm_quant(x, r, gamma, EPS, added=t), lambda t: lce.add_rmsnorm_backward(dy, None, x, r, gamma, rstd, grad_hidden=t),
+                 lambda t: lce.clip_grad_norm(x, 1.0, out=t), lambda t: lce.clip_grad_norm([t], 1.0, out=[t])):
+        t = followed()
+        with pytest.raises(ValueError):
+            call(t)
+        assert torch.equal(t, x)
+        with torch.no_grad():
+            call(t)
+            assert not torch.equal(t, x)
+        call(followed().detach())
