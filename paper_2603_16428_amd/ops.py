@@ -224,7 +224,7 @@ def add_rmsnorm_backward(grad_normed, grad_added, hidden, residual, gamma, rstd,
         _check_like(grad_added, shape, dtype, dev, "grad_added")
     if residual is not None:
         _check_like(residual, shape, dtype, dev, "residual")
-    if rstd.shape != shape[:-1] or rstd.dtype != torch.float32 or rstd.device != dev or not rstd.is_contiguous():
+    if rstd.shape != shape[:-1] or rstd.dtype != torch.float32 or rstd.device != dev or not rstd.is_contiguous() or rstd.is_neg():
         raise ValueError("rstd must be the forward call's")
     dx, dx_pitch = _output(grad_hidden, hidden, dtype, "grad_hidden")
     dg = ws = None

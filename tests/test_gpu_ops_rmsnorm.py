@@ -523,6 +523,17 @@ def test_refusals(lce):
     assert e.value.status == 2
 
 
+def test_lazily_negated_rstd_is_refused(lce):
+    """Its bytes have the other sign: the gradients would too."""
+    x, r, gamma, dy, ds = _inputs(4, 64, "fp32")
+    _, _, rstd = lce.add_rmsnorm_forward(x, r, gamma, EPS, return_rstd=True)
+    lazy = torch._neg_view(-rstd)
+    assert torch.equal(lazy, rstd)
+    with pytest.raises(ValueError):
+        lce.add_rmsnorm_backward(dy, ds, x, r, gamma, lazy)
+    _check_backward(*lce.add_rmsnorm_backward(dy, ds, x, r, gamma, lazy.resolve_neg()), dy, ds, x, r, gamma, rstd)
+
+
 def test_streams_and_graphs(lce):
     """On a side stream; captured and replayed with eager work between, on inputs changed in place; two graphs
     with a workspace each, replayed in turn."""
