@@ -155,6 +155,28 @@ def test_in_place(lce, H):
         assert got is ins[k] and torch.equal(got, dx) and torch.equal(gg, dg)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("H", [5, 129, 257, 513, 1025, 1543, 2049, 4097, 6151, 8199, 12289, 16385, 32761])
+def test_in_place_of_odd_widths(lce, H, dtype):
+    """A row's last values are loaded with some of the thread's before (of another wave, where H is just above a
+    multiple of 512): in place they are the old ones all the same, in both directions, with rows back to back."""
+    x, r, gamma, dy, ds = _inputs(33, H, dtype, seed=4)
+    want = lce.add_rmsnorm_forward(x, r, gamma, EPS, return_rstd=True)
+    for k in range(2):
+        ins = [x.clone(), r.clone()]
+        got = lce.add_rmsnorm_forward(*ins, gamma, EPS, normed=ins[k], added=ins[1 - k])
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    q = lce.add_rmsnorm_quant(x, r, gamma, EPS, 64)
+    a = x.clone()
+    got = lce.add_rmsnorm_quant(a, r, gamma, EPS, 64, added=a)
+    assert got[2] is a and torch.equal(a, q[2]) and torch.equal(got[0].view(torch.uint8), q[0].view(torch.uint8))
+    dx, dg = lce.add_rmsnorm_backward(dy, ds, x, r, gamma, want[2])
+    for k in range(4):
+        ins = [dy.clone(), ds.clone(), x.clone(), r.clone()]
+        got, gg = lce.add_rmsnorm_backward(*ins, gamma, want[2], grad_hidden=ins[k])
+        assert got is ins[k] and torch.equal(got, dx) and torch.equal(gg, dg)
+
+
 def test_rows_that_are_not_finite_or_zero(lce):
     x, r, gamma, _, _ = _inputs(12, 1000, "bf16")
     clean = lce.add_rmsnorm_forward(x, r, gamma, EPS)
