@@ -19,6 +19,7 @@ EXPORTED = ("lce_add_rmsnorm_forward", "lce_add_rmsnorm_quant", "lce_add_rmsnorm
 FP8 = torch.float8_e4m3fn
 GROUP_SIZES = (0, 32, 64, 128)
 NORM_TYPES = {2.0: 0, float("inf"): 1}
+_PLAIN = {torch.Tensor}
 
 _lib = None
 
@@ -330,14 +331,14 @@ def _dense(t) -> bool:
 
 
 def _check_grads(grads):
-    """The gradients that are not None, their device, and their lce_tensor_t entries."""
+    """The gradients that are not None, their device, their lce_tensor_t entries, and whether one requires a gradient."""
     grads = [grads] if isinstance(grads, torch.Tensor) else [g for g in grads if g is not None]
     if not grads:
         raise ValueError("no gradients")
     index, flat = grads[0].get_device(), []
     if index < 0:
         raise ValueError("gradients must be device tensors")
-    strided, codes = torch.strided, DTYPES
+    strided, codes, requires = torch.strided, DTYPES, False
     for g in grads:  # a model has hundreds: half a microsecond for each
         code = codes.get(g.dtype)
         if code is None or g.layout is not strided or g.is_neg():
@@ -346,8 +347,14 @@ def _check_grads(grads):
             raise ValueError("gradients must be tensors of one device")
         if not (g.is_contiguous() or g.numel() == 0 or _dense(g)):
             raise ValueError("a gradient's values must fill one block of memory, in any order")
+        if g.requires_grad:
+            requires = True
         flat += (g.data_ptr(), g.numel(), code)
-    return grads, grads[0].device, array.array("q", flat)
+    return grads, grads[0].device, array.array("q", flat), requires
+
+
+def _followed(grads, requires) -> bool:
+    return (requires or getattr(torch.autograd.forward_ad, "_current_level", 0) >= 0) and _differentiated(grads)
 
 
 class _Undifferentiated(torch.autograd.Function):
@@ -385,19 +392,22 @@ def grad_norm(grads, norm_type: float = 2.0, workspace: torch.Tensor | None = No
     norm raises if it is differentiated.
     """
     kind = _norm_type(norm_type)
-    grads, dev, table = _check_grads(grads)
+    grads, dev, table, requires = _check_grads(grads)
+    if _followed(grads, requires):
+        return _Undifferentiated.apply(lambda: _norm(grads, dev, table, kind, workspace), *grads)
+    return _norm(grads, dev, table, kind, workspace)
 
-    def call():
-        norm = grads[0].new_empty((), dtype=torch.float32)
-        ws = _space(workspace, grads[0], grad_norm_workspace_size(len(grads)))
-        _call("lce_grad_norm", dev, table.buffer_info()[0], len(grads), kind, norm.data_ptr(), ws.data_ptr(), ws.numel())
-        return norm
 
-    return _Undifferentiated.apply(call, *grads) if _differentiated(grads) else call()
+def _norm(grads, dev, table, norm_type, workspace):
+    norm = grads[0].new_empty((), dtype=torch.float32)
+    ws = _space(workspace, grads[0], grad_norm_workspace_size(len(grads)))
+    _call("lce_grad_norm", dev, table.buffer_info()[0], len(grads), norm_type, norm.data_ptr(), ws.data_ptr(), ws.numel())
+    return norm
 
 
 def _clip(grads, dev, table, max_norm, norm_type, out, workspace):
-    if any(issubclass(c, torch.nn.Parameter) for c in set(map(type, grads))):  # scaling the weights themselves is never meant
+    kinds = set(map(type, grads))
+    if kinds != _PLAIN and any(issubclass(c, torch.nn.Parameter) for c in kinds):  # scaling the weights themselves is never meant
         raise ValueError("clipping takes gradients, not parameters: [p.grad for p in parameters]")
     norm = grads[0].new_empty((), dtype=torch.float32)
     ws = _space(workspace, grads[0], grad_norm_workspace_size(len(grads)))
@@ -418,8 +428,8 @@ def clip_grad_norm_(grads, max_norm: float, norm_type: float = 2.0, workspace: t
     of their own keep the one they had.
     """
     kind = _norm_type(norm_type)
-    grads, dev, table = _check_grads(grads)
-    if any([g.is_leaf for g in grads if g.requires_grad]):
+    grads, dev, table, requires = _check_grads(grads)
+    if requires and any(g.requires_grad and g.is_leaf for g in grads):
         raise ValueError("a leaf that requires a gradient is a weight, not a gradient: [p.grad for p in parameters]")
     return _clip(grads, dev, table, max_norm, kind, None, workspace)
 
@@ -432,19 +442,29 @@ def clip_grad_norm(grads, max_norm: float, norm_type: float = 2.0, out=None, wor
     with a graph of their own the norm and new tensors raise if they are differentiated.
     """
     kind = _norm_type(norm_type)
-    grads, dev, table = _check_grads(grads)
+    grads, dev, table, requires = _check_grads(grads)
     if out is not None:
         out = [out] if isinstance(out, torch.Tensor) else [t for t in out if t is not None]
-        if len(out) != len(grads) or any(t.shape != g.shape or t.dtype != g.dtype or t.device != dev
-                                         or (t.stride() != g.stride() and t.numel() > 1) or t.is_neg() for t, g in zip(out, grads)):
+        index, same = dev.index, len(out) == len(grads)
+        for t, g in zip(out, grads):  # half a microsecond for each, as in _check_grads
+            if (t.get_device() != index or t.dtype is not g.dtype or t.shape != g.shape or t.is_neg()
+                    or not (t.is_contiguous() and g.is_contiguous() or t.stride() == g.stride() or t.numel() <= 1)):
+                same = False
+            if t.requires_grad:
+                _check_unfollowed(t, "out")
+        if not same:
             raise ValueError("out must match the gradients in number, shape, strides, dtype and device")
-        for t in out:
-            _check_unfollowed(t, "out")
+    if _followed(grads, requires):
+        norm, *new = _Undifferentiated.apply(lambda: _clip_into(grads, dev, table, max_norm, kind, out, workspace), *grads)
+        return norm, new if out is None else out
+    if out is None:
+        norm, *out = _clip_into(grads, dev, table, max_norm, kind, None, workspace)
+        return norm, out
+    return _clip(grads, dev, table, max_norm, kind, out, workspace), out
 
-    def call():
-        outs = [torch.empty_like(g) for g in grads] if out is None else out
-        norm = _clip(grads, dev, table, max_norm, kind, outs, workspace)
-        return (norm, *outs) if out is None else (norm,)
 
-    norm, *new = _Undifferentiated.apply(call, *grads) if _differentiated(grads) else call()
-    return norm, new if out is None else out
+def _clip_into(grads, dev, table, max_norm, norm_type, out, workspace):
+    """The norm, and the clipped gradients where they are new."""
+    outs = [torch.empty_like(g) for g in grads] if out is None else out
+    norm = _clip(grads, dev, table, max_norm, norm_type, outs, workspace)
+    return (norm,) if out is not None else (norm, *outs)
