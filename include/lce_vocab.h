@@ -1,0 +1,53 @@
+/*
+ * lce_vocab.h -- C ABI of the operators on the vocabulary's matrix and logits beside the output-layer step (lce.h) for
+ * MI355X (gfx950): the embedding lookup and its gradient, rows and weights in 4 bits and their product, and the choice
+ * of a token from logits.
+ *
+ * Conventions are those of lce_ops.h: device pointers owned by the caller, work enqueued in order on `stream`, which
+ * belongs to the current device, no allocation and no synchronisation, arguments validated before anything is enqueued,
+ * deterministic results; tensors need only their element type's alignment unless noted; row tensors have a pitch of their
+ * own (`*_ld`, elements between rows): any for an input, 0 included, at least the row's length for an output; no rows are
+ * a call that does nothing. Outputs overlap neither inputs nor each other, else LCE_ERR_INVALID_ARGUMENT.
+ */
+#ifndef LCE_VOCAB_H_
+#define LCE_VOCAB_H_
+
+#include "lce.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * out_i = scale weight_{t_i}, in fp32, rounded once. A token outside [0, V) gives a row of NaN and reads nothing.
+ *   tokens      : device [N], integers of token_bytes (4 or 8) bytes.
+ *   weight      : device [V,H] of dtype, 1 <= V < 2^31, 1 <= H <= LCE_EMBEDDING_MAX_H.
+ *   scale       : finite.
+ *   out         : device [N,H] of dtype.
+ */
+#define LCE_EMBEDDING_MAX_H (1 << 20)
+lce_status_t lce_embedding_forward(const void* tokens, int token_bytes, int64_t N, const void* weight, int64_t weight_ld,
+                                   int64_t V, int64_t H, int dtype, float scale, void* out, int64_t out_ld, void* stream);
+
+/*
+ * The gradient of weight: for each v, scale times the sum of grad's rows whose token is v, in fp32 in an order that the tokens
+ * alone fix, rounded once.
+ *   grad        : device [N,H] of dtype, N <= LCE_EMBEDDING_MAX_N.
+ *   padding_idx : a token whose rows count for nothing, or -1. Tokens outside [0, V) count for nothing either.
+ *   grad_weight : device [V,H] of dtype. accumulate = 0: all of it is written, zeros where no token points. Otherwise the sum is
+ *                 added to the value there (in fp32, rounded once), and only rows that a counting token names are touched.
+ *   workspace   : device memory of lce_embedding_workspace_size(N, H) bytes, 256-byte aligned. The size does not
+ *                 fall as N or H grows. Calls (and captured graphs) that may run at the same time need one each.
+ */
+#define LCE_EMBEDDING_MAX_N (1 << 28)
+size_t lce_embedding_workspace_size(int64_t N, int64_t H);
+lce_status_t lce_embedding_backward(const void* grad, int64_t grad_ld, const void* tokens, int token_bytes, int64_t N,
+                                    int64_t V, int64_t H, int dtype, float scale, int64_t padding_idx, void* grad_weight,
+                                    int64_t grad_weight_ld, int accumulate, void* workspace, size_t workspace_bytes,
+                                    void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* LCE_VOCAB_H_ */

@@ -8,10 +8,12 @@ from .lce import (AdamConfig, HeadState, HeadStepTiming, LCEError, LinearCrossEn
 from .ops import (AddRMSNorm, add_rmsnorm, add_rmsnorm_backward, add_rmsnorm_forward, add_rmsnorm_quant,
                   add_rmsnorm_workspace_size, clip_grad_norm, clip_grad_norm_, grad_norm, grad_norm_workspace_size,
                   rmsnorm)
+from .vocab import Embedding, embedding, embedding_backward, embedding_forward, embedding_workspace_size
 
-__all__ = ["AdamConfig", "AddRMSNorm", "HeadState", "HeadStepTiming", "LCEError", "LinearCrossEntropy", "PlanInfo",
+__all__ = ["AdamConfig", "AddRMSNorm", "HeadState", "HeadStepTiming", "LCEError", "LinearCrossEntropy", "Embedding", "PlanInfo",
            "RMSNormLinearCrossEntropy", "add_rmsnorm", "add_rmsnorm_backward", "add_rmsnorm_forward",
            "add_rmsnorm_quant", "add_rmsnorm_workspace_size", "auto_chunk_tokens", "clip_grad_norm", "clip_grad_norm_",
+           "embedding", "embedding_backward", "embedding_forward", "embedding_workspace_size",
            "forward", "forward_backward", "forward_no_alloc", "grad_norm", "grad_norm_workspace_size",
            "head_train_step",
            "host_adam_step", "linear_cross_entropy", "load_library", "plan_info", "rmsnorm", "rmsnorm_forward",

@@ -3,7 +3,8 @@
     python -m paper_2603_16428_amd.build
 
 compiles csrc/lce_api.hip (which includes the step's kernels), csrc/ops_api.hip (the operators around
-the step) and csrc/host_adam.cpp (the host optimizer step) into liblce.so next to this file.
+the step), csrc/vocab_api.hip (those on the vocabulary's matrix and logits) and csrc/host_adam.cpp (the host
+optimizer step) into liblce.so next to this file.
 """
 from __future__ import annotations
 
@@ -17,8 +18,9 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "liblce.so")
 KERNEL_SOURCES = [os.path.join(HERE, "csrc", "lce_api.hip")]
 OPS_SOURCES = [os.path.join(HERE, "csrc", "ops_api.hip")]
+VOCAB_SOURCES = [os.path.join(HERE, "csrc", "vocab_api.hip")]
 HOST_SOURCES = [os.path.join(HERE, "csrc", "host_adam.cpp")]
-SOURCES = KERNEL_SOURCES + OPS_SOURCES + HOST_SOURCES
+SOURCES = KERNEL_SOURCES + OPS_SOURCES + VOCAB_SOURCES + HOST_SOURCES
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -1,0 +1,174 @@
+"""Python binding of the operators on the vocabulary's matrix and logits (include/lce_vocab.h).
+
+In front of a model: the rows of its V x H matrix that tokens name, and their gradient, alone or added to that of an output
+layer with the same weight. Argument marshalling only, as in lce.py and ops.py: every computation runs in liblce.so's HIP
+kernels, on the current stream of the tensors' device, and nothing waits for the GPU.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import torch
+
+from . import ops
+from .lce import DTYPES, LCEError, load_library
+from .ops import _check_unfollowed, _pitch, _space, _upstream, _written
+
+EXPORTED = ("lce_embedding_forward", "lce_embedding_workspace_size", "lce_embedding_backward")
+_TOKENS = {torch.int64: 8, torch.int32: 4}
+
+_lib = None
+
+
+def _library() -> ctypes.CDLL:
+    global _lib
+    if _lib is not None:
+        return _lib
+    lib = load_library()
+    i64, vp, sz, ci, f32 = ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
+    for name, args, res in [
+            ("lce_embedding_forward", [vp, ci, i64, vp, i64, i64, i64, ci, f32, vp, i64, vp], ci),
+            ("lce_embedding_workspace_size", [i64, i64], sz),
+            ("lce_embedding_backward", [vp, i64, vp, ci, i64, i64, i64, ci, f32, i64, vp, i64, ci, vp, sz, vp], ci)]:
+        f = getattr(lib, name)
+        f.argtypes, f.restype = args, res
+    _lib = lib
+    return lib
+
+
+def _call(name: str, device, *args) -> None:
+    if _lib is None:
+        _library()
+    ops._call(name, device, *args)
+
+
+def _device_rows(t, what: str):
+    """The device of rows in one of the three types."""
+    if not t.is_cuda:
+        raise ValueError(f"{what} must be a device tensor")
+    if t.dtype not in DTYPES:
+        raise ValueError(f"{what} must be bfloat16, float16 or float32")
+    if t.is_neg():
+        raise ValueError(f"{what} is a lazily negated view: resolve_neg() it first")
+    return t.device
+
+
+def _given(t, shape, dtype, dev, what: str):
+    """A given output, checked and told to autograd as written."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != dev.index:
+        raise ValueError(f"{what} must be {list(shape)} of {dtype} on {dev}")
+    if t.is_neg():
+        raise ValueError(f"{what} is a lazily negated view: resolve_neg() it first")
+    _check_unfollowed(t, what)
+    _written([t])
+    return t
+
+
+# ---- embedding -----------------------------------------------------------------------------------
+
+def _check_tokens(tokens, dev):
+    """Bytes of a token."""
+    if tokens.get_device() != dev.index:
+        raise ValueError("tokens must be on the device of the rows")
+    size = _TOKENS.get(tokens.dtype)
+    if size is None or not tokens.is_contiguous():
+        raise ValueError("tokens must be contiguous int64 or int32")
+    return size
+
+
+def _check_scale(scale):
+    if not math.isfinite(scale):
+        raise ValueError("scale must be finite")
+
+
+def embedding_forward(tokens, weight, scale: float = 1.0, out=None):
+    """scale * weight[tokens]: [..., H] of weight's type, each value rounded once.
+
+    tokens [...] (int64 or int32), weight [V, H] with consecutive values in a row. A token outside [0, V) gives a row of NaN.
+    Not differentiable: see embedding.
+    """
+    dev = _device_rows(weight, "weight")
+    if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
+        raise ValueError("weight must be [V, H]")
+    size = _check_tokens(tokens, dev)
+    _check_scale(scale)
+    V, H = weight.shape
+    shape = tokens.shape + (H,)
+    if out is None:
+        out, pitch = weight.new_empty(shape), H
+    else:
+        pitch = _pitch(_given(out, shape, weight.dtype, dev, "out"), "out")
+    _call("lce_embedding_forward", dev, tokens.data_ptr(), size, tokens.numel(), weight.data_ptr(), _pitch(weight, "weight"), V, H,
+          DTYPES[weight.dtype], scale, out.data_ptr(), pitch)
+    return out
+
+
+def embedding_workspace_size(N: int, H: int) -> int:
+    """Bytes of workspace for the gradient of N tokens' rows."""
+    return int((_lib or _library()).lce_embedding_workspace_size(N, H))
+
+
+def embedding_backward(grad, tokens, num_embeddings: int, scale: float = 1.0, padding_idx: int | None = None, grad_weight=None,
+                       accumulate: bool = False, workspace: torch.Tensor | None = None):
+    """The gradient of the weight, [num_embeddings, H]: for each token, scale times the sum of its rows of grad [..., H].
+
+    Sums are fp32 in an order that the tokens fix, rounded once. grad_weight may be given; with accumulate the sums are added
+    to the values there (that of linear_cross_entropy where the output layer has the same weight), and only the rows
+    that tokens name are read and written. Rows of padding_idx, and of tokens outside the matrix, count for nothing.
+    """
+    dev = _device_rows(grad, "grad")
+    size = _check_tokens(tokens, dev)
+    _check_scale(scale)
+    if grad.dim() < 1 or grad.shape[:-1] != tokens.shape or grad.shape[-1] < 1:
+        raise ValueError("grad must be [..., H] with a row for each token")
+    if num_embeddings < 1 or (padding_idx is not None and not 0 <= padding_idx < num_embeddings):
+        raise ValueError("padding_idx must be a token of the matrix, which has at least one row")
+    N, H = tokens.numel(), grad.shape[-1]
+    if grad_weight is None:
+        if accumulate:
+            raise ValueError("accumulate adds to a given grad_weight")
+        grad_weight, pitch = grad.new_empty((num_embeddings, H)), H
+    else:
+        pitch = _pitch(_given(grad_weight, (num_embeddings, H), grad.dtype, dev, "grad_weight"), "grad_weight")
+    need = (_lib or _library()).lce_embedding_workspace_size(N, H)
+    if need == 0:
+        raise LCEError(2, "lce_embedding_workspace_size")
+    ws = _space(workspace, grad, need)
+    _call("lce_embedding_backward", dev, grad.data_ptr(), _pitch(grad, "grad"), tokens.data_ptr(), size, N, num_embeddings, H,
+          DTYPES[grad.dtype], scale, -1 if padding_idx is None else padding_idx, grad_weight.data_ptr(), pitch, int(accumulate),
+          ws.data_ptr(), ws.numel())
+    return grad_weight
+
+
+class Embedding(torch.autograd.Function):
+    """embedding_forward with the gradient of weight, a dense tensor."""
+
+    @staticmethod
+    def forward(ctx, tokens, weight, scale, padding_idx):
+        ctx.set_materialize_grads(False)
+        if padding_idx is not None and not 0 <= padding_idx < len(weight):
+            raise ValueError("padding_idx must be a token of the matrix")
+        ctx.save_for_backward(tokens)
+        ctx.call = len(weight), scale, padding_idx
+        return embedding_forward(tokens, weight, scale)
+
+    @staticmethod
+    def backward(ctx, grad):
+        if torch.is_grad_enabled():  # under create_graph: the gradient says so if it is differentiated again
+            return Embedding._once(ctx, grad)
+        return Embedding._gradients(ctx, grad)
+
+    @staticmethod
+    def _gradients(ctx, grad):
+        if grad is None or not ctx.needs_input_grad[1]:
+            return None, None, None, None
+        tokens, = ctx.saved_tensors
+        return None, embedding_backward(_upstream(grad), tokens, *ctx.call), None, None
+
+    _once = staticmethod(torch.autograd.function.once_differentiable(_gradients.__func__))
+
+
+def embedding(tokens, weight, scale: float = 1.0, padding_idx: int | None = None):
+    """scale * weight[tokens]. Differentiable (once) with respect to weight; rows of padding_idx get no gradient."""
+    return Embedding.apply(tokens, weight, scale, padding_idx)
