@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void embedding_kernel(const EmbedArgs a) {
 
 // ---- the positions sorted by token ----
 
-constexpr int kSortThreads = 1024, kSortEach = 4, kSortTile = kSortThreads * kSortEach, kSortWaves = kSortThreads / 64;
+constexpr int kSortThreads = 1024, kSortEach = 2, kSortTile = kSortThreads * kSortEach, kSortWaves = kSortThreads / 64;
 constexpr int kSortBits = 6, kSortBins = 1 << kSortBits;
 static_assert(kSortBins * kSortWaves == kSortThreads, "one count per thread");
 
@@ -196,8 +196,52 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(const Sort
 
 constexpr int kMergeRuns = 16;
 
-// Up to 16 runs of `length` (a power of two) become one: an element's place is its own and, in each other run, the
-// number of elements that come before it, found in all runs at once.
+// Up to RUNS tiles become one run: an element's place is its own and, in each other tile, the number of elements that come
+// before it, found in all tiles at once in a copy of their keys in LDS (8192 positions: 21 us searched in memory).
+template <int RUNS>
+__global__ __launch_bounds__(256) void embedding_merge_tiles_kernel(const uint32_t* __restrict__ key, const uint32_t* __restrict__ at,
+                                                                    uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out,
+                                                                    int64_t N) {
+  constexpr int kKeys = RUNS * kSortTile, kLoads = kKeys / 1024;
+  __shared__ uint32_t keys[kKeys];
+  const int64_t p = (int64_t)blockIdx.x * 256 + threadIdx.x, group = (int64_t)blockIdx.x * 256 / kKeys * kKeys;
+  const int left = (int)(N - group < kKeys ? N - group : kKeys);
+  u32x4 k4[kLoads];  // (the arrays' lengths are multiples of 64)
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) __builtin_memcpy(&k4[u], key + group + min(u * 1024 + (int)threadIdx.x * 4, (left - 1) / 4 * 4), 16);
+#pragma unroll
+  for (int u = 0; u < kLoads; ++u) *(u32x4*)&keys[u * 1024 + threadIdx.x * 4] = k4[u];
+  const uint32_t place = at[p < N ? p : N - 1];
+  __syncthreads();
+  if (p >= N) return;
+  const int self = (int)(p - group), own = self / kSortTile;
+  const uint32_t k = keys[self];
+  int lo[RUNS];
+#pragma unroll
+  for (int b = 0; b < RUNS; ++b) lo[b] = b * kSortTile;
+  // Without a branch, so that a step is one read's latency.
+  for (int step = kSortTile; step > 0; step >>= 1) {
+    uint32_t other[RUNS];
+#pragma unroll
+    for (int b = 0; b < RUNS; ++b) {
+      const int next = lo[b] + step;
+      other[b] = keys[next <= min(left, (b + 1) * kSortTile) ? next - 1 : self];
+    }
+#pragma unroll
+    for (int b = 0; b < RUNS; ++b) {
+      const int next = lo[b] + step;
+      if (next <= min(left, (b + 1) * kSortTile) && (b < own ? other[b] <= k : other[b] < k)) lo[b] = next;
+    }
+  }
+  int to = self % kSortTile;
+#pragma unroll
+  for (int b = 0; b < RUNS; ++b)
+    if (b != own) to += lo[b] - b * kSortTile;
+  key_out[group + to] = k;
+  at_out[group + to] = place;
+}
+
+// The same for up to 16 longer runs, of `length` (a power of two), in memory.
 __global__ __launch_bounds__(256) void embedding_merge_kernel(const uint32_t* __restrict__ key, const uint32_t* __restrict__ at,
                                                               uint32_t* __restrict__ key_out, uint32_t* __restrict__ at_out,
                                                               int64_t N, int64_t length) {
@@ -213,14 +257,24 @@ __global__ __launch_bounds__(256) void embedding_merge_kernel(const uint32_t* __
     const int64_t left = N - group - b * length;
     len[b] = b == own || left < 0 ? 0 : left < length ? left : length;
   }
-  for (int64_t step = length; step > 0; step >>= 1) {
+  // Three of a run's elements a step, those of all runs requested together without a branch (a place past the run's
+  // end reads another and counts for nothing): a step is a load's latency.
+  for (int64_t step = __builtin_ctzll(length) % 2 == 0 ? length : length / 2; step > 0; step >>= 2) {  // powers of four
+    uint32_t other[kMergeRuns][3];
+#pragma unroll
+    for (int b = 0; b < kMergeRuns; ++b)
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        const int64_t next = lo[b] + (q + 1) * step;
+        other[b][q] = key[next <= len[b] ? group + b * length + next - 1 : p];
+      }
 #pragma unroll
     for (int b = 0; b < kMergeRuns; ++b) {
-      const int64_t next = lo[b] + step;
-      if (next <= len[b]) {
-        const uint32_t other = key[group + b * length + next - 1];
-        if (b < own ? other <= k : other < k) lo[b] = next;
-      }
+      int more = 0;
+#pragma unroll
+      for (int q = 0; q < 3; ++q)
+        more += lo[b] + (q + 1) * step <= len[b] && (b < own ? other[b][q] <= k : other[b][q] < k);
+      lo[b] += more * step;
     }
   }
   int64_t to = p - own * length;
@@ -240,78 +294,96 @@ struct EmbedSumArgs {
   int64_t grad_ld, out_ld, part_ld;
   int64_t N;
   uint32_t V;
-  int H, chunk, accumulate;
+  int H, chunk;
   float scale;
 };
 
-template <RowEnd END, typename T>
-__device__ __forceinline__ void write_sum(const EmbedSumArgs& a, uint32_t v, int c, const float (&sum)[kNormVec]) {
-  T* p = (T*)a.out + (int64_t)v * a.out_ld + c;
+template <RowEnd END, bool ADD, typename T>
+__device__ __forceinline__ void write_sum(const EmbedSumArgs& a, uint32_t v, int c, const float (&sum)[kNormVec], RawRow<T>& old) {
   const int n = a.H - c;
-  RawRow<T> old;
-  old.clear();
-  if (a.accumulate) {
-    load_raw<END>(p, n, old);
-    align_end<END>(n, old);
-  }
   float y[kNormVec];
+  if constexpr (ADD) {
+    align_end<END>(n, old);
 #pragma unroll
-  for (int e = 0; e < kNormVec; ++e) y[e] = fmaf(sum[e], a.scale, old.at(e));
-  store_row<END>(p, n, y);
+    for (int e = 0; e < kNormVec; ++e) y[e] = fmaf(sum[e], a.scale, old.at(e));
+  } else {
+#pragma unroll
+    for (int e = 0; e < kNormVec; ++e) y[e] = sum[e] * a.scale;
+  }
+  store_row<END>((T*)a.out + (int64_t)v * a.out_ld + c, n, y);
 }
 
-// TPR threads walk along a chunk of the sorted positions, 8 columns each, eight rows requested at once.
-template <typename T, int TPR, RowEnd END>
+constexpr int kMostChunk = 64;
+
+// TPR threads walk along a chunk of the sorted positions, 8 columns each. Bound by the loads' latency unless many are on
+// the way: the chunk's tokens and positions come first, all at once, and then eight rows are requested ahead
+// (with the row's earlier value behind the last row of a run, where it is added to).
+template <typename T, int TPR, RowEnd END, bool ADD>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbedSumArgs a) {
-  constexpr int kAhead = 8;
-  int64_t b = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  const int64_t first = b * a.chunk;
-  if (first >= a.N) return;
-  const int n = (int)(a.N - first < a.chunk ? a.N - first : a.chunk);
+  constexpr int kAhead = 8, kChunks = 256 / TPR;
+  __shared__ uint32_t keys[kChunks][kMostChunk + 1], places[kChunks][kMostChunk];
+  const int64_t b0 = (int64_t)blockIdx.x * kChunks;
+  for (int k = threadIdx.x; k < kChunks * (a.chunk + 1); k += 256) {
+    const int of = k / (a.chunk + 1), j = k % (a.chunk + 1);
+    const int64_t p = (b0 + of) * a.chunk + j;
+    keys[of][j] = p < a.N ? a.key[p] : a.V;
+    if (j < a.chunk) places[of][j] = p < a.N ? a.at[p] : 0u;
+  }
+  __syncthreads();
+  int group = threadIdx.x / TPR;
+  if constexpr (TPR >= 64) group = __builtin_amdgcn_readfirstlane(group);  // (what a wave shares is a scalar)
+  const int64_t b = b0 + group, first = b * a.chunk;
   const int c = (blockIdx.y * TPR + threadIdx.x % TPR) * kNormVec;
-  if (c >= a.H) return;
-  float acc[kNormVec] = {};
-  uint32_t now = a.key[first];
-  // Whether the run at hand began in an earlier chunk.
-  bool begun = first > 0 && a.key[first - 1] == now;
-  auto leave = [&](int slot) {
-    float* p = a.part + (b * 2 + slot) * a.part_ld + c;
-    __builtin_memcpy(p, acc, sizeof(acc));
-  };
-  for (int j0 = 0; j0 < n; j0 += kAhead) {
-    uint32_t k[kAhead];
-    RawRow<T> g[kAhead];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) k[u] = j0 + u < n ? a.key[first + j0 + u] : a.V;
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      g[u].clear();
-      if (k[u] < a.V) load_raw<END>((const T*)a.grad + (int64_t)a.at[first + j0 + u] * a.grad_ld + c, a.H - c, g[u]);
+  if (first >= a.N || c >= a.H) return;
+  const int n = (int)(a.N - first < a.chunk ? a.N - first : a.chunk);
+  auto scalar = [](uint32_t v) { return TPR >= 64 ? (uint32_t)__builtin_amdgcn_readfirstlane((int)v) : v; };
+  auto key = [&](int j) { return scalar(keys[group][j]); };
+  RawRow<T> g[kAhead], old[kAhead];
+  // No branch stands around a request (of places past the chunk the last row is read again): behind one, the compiler
+  // waits for all that is on the way.
+  auto request = [&](int j, RawRow<T>& row, RawRow<T>& before) {
+    j = j < n ? j : n - 1;
+    load_raw<END>((const T*)a.grad + (int64_t)scalar(places[group][j]) * a.grad_ld + c, a.H - c, row);
+    if constexpr (ADD) {
+      const uint32_t v = key(j);
+      load_raw<END>((const T*)a.out + (int64_t)(v < a.V ? v : 0u) * a.out_ld + c, a.H - c, before);
     }
+  };
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) request(u, g[u], old[u]);
+  float acc[kNormVec] = {};
+  // Whether the run at hand began in an earlier chunk.
+  bool begun = first > 0 && a.key[first - 1] == key(0);
+  auto leave = [&](int slot) { __builtin_memcpy(a.part + (b * 2 + slot) * a.part_ld + c, acc, sizeof(acc)); };
+  for (int j0 = 0; j0 < n; j0 += kAhead) {
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      if (j0 + u >= n) break;
-      if (k[u] != now) {
-        if (begun) leave(0);
-        else write_sum<END, T>(a, now, c, acc);
-        begun = false;
-        now = k[u];
+      const int j = j0 + u;
+      if (j < n) {
+        align_end<END>(a.H - c, g[u]);
 #pragma unroll
-        for (int e = 0; e < kNormVec; ++e) acc[e] = 0.f;
+        for (int e = 0; e < kNormVec; ++e) acc[e] += g[u].at(e);
+        const uint32_t v = key(j);
+        const bool goes_on = key(j + 1) == v;
+        if (!goes_on || j + 1 == n) {
+          // (a.V is no token: rows that count for nothing, sorted last)
+          if (v < a.V) {
+            if (begun) leave(0);
+            else if (goes_on) leave(1);
+            else write_sum<END, ADD, T>(a, v, c, acc, old[u]);
+          }
+          begun = false;
+#pragma unroll
+          for (int e = 0; e < kNormVec; ++e) acc[e] = 0.f;
+        }
       }
-      if (now >= a.V) return;  // sorted last: nothing that counts follows
-      align_end<END>(a.H - c, g[u]);
-#pragma unroll
-      for (int e = 0; e < kNormVec; ++e) acc[e] += g[u].at(e);
+      request(j + kAhead, g[u], old[u]);
     }
   }
-  if (begun) leave(0);
-  else if (first + n < a.N && a.key[first + n] == now) leave(1);
-  else write_sum<END, T>(a, now, c, acc);
 }
 
 // A workgroup for each chunk that a run begins in and leaves: the run's sums from its chunks, in their order.
-template <typename T, RowEnd END>
+template <typename T, RowEnd END, bool ADD>
 __global__ __launch_bounds__(256) void embedding_join_kernel(const EmbedSumArgs a) {
   const int64_t b = blockIdx.x, first = b * a.chunk, next = first + a.chunk;
   if (next >= a.N) return;
@@ -353,7 +425,9 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const EmbedSumArgs 
   }
 #pragma unroll
   for (int e = 0; e < kNormVec; ++e) acc[e] += lost[e];
-  write_sum<END, T>(a, v, c, acc);
+  RawRow<T> old;
+  if constexpr (ADD) load_raw<END>((const T*)a.out + (int64_t)v * a.out_ld + c, a.H - c, old);
+  write_sum<END, ADD, T>(a, v, c, acc, old);
 }
 
 }  // namespace lce

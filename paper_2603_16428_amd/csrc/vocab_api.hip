@@ -74,7 +74,7 @@ FillArgs fill_of(void* p, int64_t ld, int64_t V, int64_t H, int64_t size) {
   return {(char*)p, kPiece, kPiece, bytes - (pieces - 1) * kPiece, pieces};
 }
 
-template <typename T>
+template <typename T, bool ADD>
 lce_status_t run_embedding_backward(const SortArgs& sort0, const FillArgs& fill, const EmbedSumArgs& sum0, const EmbedSpace& w, hipStream_t s) {
   SortArgs sort = sort0;
   EmbedSumArgs sum = sum0;
@@ -86,9 +86,17 @@ lce_status_t run_embedding_backward(const SortArgs& sort0, const FillArgs& fill,
     hipLaunchKernelGGL(embedding_sort_kernel, dim3((unsigned)(sort.tiles + fills)), dim3(kSortThreads), 0, s, sort, fill);
   if (sort.N == 0) return launched();
   int now = 0;
-  for (int64_t length = kSortTile; length < sort.N; length *= kMergeRuns, now ^= 1)
-    hipLaunchKernelGGL(embedding_merge_kernel, dim3((unsigned)cdiv(sort.N, 256)), dim3(256), 0, s, w.key[now], w.at[now],
-                       w.key[now ^ 1], w.at[now ^ 1], sort.N, length);
+  const dim3 each((unsigned)cdiv(sort.N, 256));
+  for (int64_t length = kSortTile; length < sort.N; length *= kMergeRuns, now ^= 1) {
+    if (length > kSortTile) {
+      hipLaunchKernelGGL(embedding_merge_kernel, each, dim3(256), 0, s, w.key[now], w.at[now], w.key[now ^ 1], w.at[now ^ 1], sort.N, length);
+      continue;
+    }
+    // As few tiles' keys in LDS, and searches in them, as there are.
+    auto kernel = sort.tiles <= 2 ? embedding_merge_tiles_kernel<2> : sort.tiles <= 4 ? embedding_merge_tiles_kernel<4>
+                : sort.tiles <= 8 ? embedding_merge_tiles_kernel<8> : embedding_merge_tiles_kernel<kMergeRuns>;
+    hipLaunchKernelGGL(kernel, each, dim3(256), 0, s, w.key[now], w.at[now], w.key[now ^ 1], w.at[now ^ 1], sort.N);
+  }
   sum.key = w.key[now];
   sum.at = w.at[now];
   const int64_t chunks = cdiv(sum.N, sum.chunk);
@@ -96,9 +104,9 @@ lce_status_t run_embedding_backward(const SortArgs& sort0, const FillArgs& fill,
     constexpr int kTpr = decltype(tpr)::value;
     constexpr RowEnd kEnd = decltype(end)::value;
     const dim3 grid((unsigned)cdiv(chunks, 256 / kTpr), (unsigned)cdiv(sum.H, kTpr * kNormVec));
-    hipLaunchKernelGGL((embedding_sum_kernel<T, kTpr, kEnd>), grid, dim3(256), 0, s, sum);
+    hipLaunchKernelGGL((embedding_sum_kernel<T, kTpr, kEnd, ADD>), grid, dim3(256), 0, s, sum);
     if (chunks > 1)
-      hipLaunchKernelGGL((embedding_join_kernel<T, kEnd>), dim3((unsigned)(chunks - 1), (unsigned)cdiv(sum.H, 256 * kNormVec)), dim3(256), 0, s, sum);
+      hipLaunchKernelGGL((embedding_join_kernel<T, kEnd, ADD>), dim3((unsigned)(chunks - 1), (unsigned)cdiv(sum.H, 256 * kNormVec)), dim3(256), 0, s, sum);
   });
   return launched();
 }
@@ -164,9 +172,13 @@ lce_status_t lce_embedding_backward(const void* grad, int64_t grad_ld, const voi
   const SortArgs sort{tokens, nullptr, nullptr, N, V, padding_idx, token_bytes == 8, 64 - __builtin_clzll((unsigned long long)V), (int)cdiv(N, kSortTile)};
   const EmbedSpace w = embed_space(workspace, N);
   const EmbedSumArgs sum{grad, grad_weight, nullptr, nullptr, w.part, grad_ld, grad_weight_ld, cdiv(H, kNormVec) * kNormVec, N,
-                         (uint32_t)V, (int)H, (int)chunk_of(N), accumulate != 0, scale};
+                         (uint32_t)V, (int)H, (int)chunk_of(N), scale};
   const FillArgs fill = accumulate ? FillArgs{} : fill_of(grad_weight, grad_weight_ld, V, H, z);
-  return by_type(dtype, [&](auto zero) { return run_embedding_backward<decltype(zero)>(sort, fill, sum, w, (hipStream_t)stream); });
+  return by_type(dtype, [&](auto zero) {
+    using T = decltype(zero);
+    return accumulate ? run_embedding_backward<T, true>(sort, fill, sum, w, (hipStream_t)stream)
+                      : run_embedding_backward<T, false>(sort, fill, sum, w, (hipStream_t)stream);
+  });
 }
 
 }  // extern "C"
