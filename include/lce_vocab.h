@@ -46,6 +46,32 @@ lce_status_t lce_embedding_backward(const void* grad, int64_t grad_ld, const voi
                                     int64_t grad_weight_ld, int accumulate, void* workspace, size_t workspace_bytes,
                                     void* stream);
 
+/*
+ * Rows in 4 bits with a scale for each 32 consecutive values (OCP MXFP4): H a multiple of 32, 32 <= H <= LCE_MXFP4_MAX_H.
+ *
+ *     scale_ig = 2^e, e = max(floor(log2(max_{j in g} |x_ij|)) - 2, -127);   code_ij = e2m1(x_ij / scale_ig)
+ *
+ * to nearest even; magnitudes above 6 become 6. A group of zeros has e = -127, one that holds a NaN or an infinity the
+ * scale byte 255 (NaN) and codes 0.
+ *   x           : device [N,H] of dtype.
+ *   codes       : device bytes [N, H/2], contiguous, 16-byte aligned: sign, two bits of exponent, one of mantissa (0, 0.5, 1,
+ *                 1.5, 2, 3, 4, 6), the first value of two in a byte's low half.
+ *   scales      : device bytes [N, H/32], contiguous: e + 127.
+ */
+#define LCE_MXFP4_MAX_H (1 << 20)
+lce_status_t lce_mxfp4_quantize(const void* x, int64_t x_ld, int64_t N, int64_t H, int dtype, void* codes, void* scales,
+                                void* stream);
+/* The values that codes and scales stand for, in dtype, rounded once (NaN in groups of scale byte 255). */
+lce_status_t lce_mxfp4_dequantize(const void* codes, const void* scales, int64_t N, int64_t H, int dtype, void* y,
+                                  int64_t y_ld, void* stream);
+/*
+ * out = X W^T for X [M,H] and W [V,H] in 4 bits, summed in fp32 and rounded once to dtype.
+ *   codes, scales : as lce_mxfp4_quantize leaves them. A group whose scale byte is 255 makes the sums that it enters NaN.
+ *   out           : device [M,V] of dtype. M, V >= 0 (M, V < 2^31).
+ */
+lce_status_t lce_mxfp4_matmul(const void* x_codes, const void* x_scales, int64_t M, const void* w_codes, const void* w_scales,
+                              int64_t V, int64_t H, int dtype, void* out, int64_t out_ld, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,374 @@
+// Rows in 4 bits with a power of two for each 32 values (OCP MXFP4), their values, and the product of two such matrices.
+//
+// A group's scale byte is the exponent of its largest magnitude less 2 (e2m1's largest power of two is 4), plus 127; its codes
+// are the values over that power, to nearest even, at most 6. Every step but that rounding is exact.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "lce_gemm16.hpp"
+#include "ops_row.hpp"
+
+namespace lce {
+
+constexpr int kMxGroup = 32;
+
+struct MxRowsArgs {
+  const void* x;  // rows (quantise)
+  void* y;        // rows (dequantise)
+  uint8_t *codes, *scales;
+  int64_t ld, N;  // the rows' pitch in elements; codes and scales are contiguous
+  int H;
+};
+
+// TPR threads a row, 8 values each, so that four neighbours share a group.
+template <typename T, int TPR>
+__global__ __launch_bounds__(256) void mxfp4_quantize_kernel(const MxRowsArgs a) {
+  constexpr int kRows = 256 / TPR, kAhead = 2;
+  const int t = threadIdx.x % TPR;
+  for (int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; i < a.N; i += (int64_t)gridDim.x * kRows) {
+    const T* p = (const T*)a.x + i * a.ld;
+    for (int c0 = t * kNormVec; c0 < a.H; c0 += kAhead * TPR * kNormVec) {
+      RawRow<T> raw[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        raw[u].clear();
+        load_raw<WHOLE>(p + c0 + u * TPR * kNormVec, a.H - c0 - u * TPR * kNormVec, raw[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int c = c0 + u * TPR * kNormVec;
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < kNormVec; ++e) top = max(top, __builtin_bit_cast(uint32_t, raw[u].at(e)) & 0x7fffffffu);
+        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+        top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+        const uint32_t e8 = top >> 23;  // 255: an infinity or a NaN
+        const uint32_t byte = e8 == 255 ? 255u : e8 > 2 ? e8 - 2 : 0u;
+        const float inv = __builtin_bit_cast(float, (254u - (e8 == 255 ? 127u : byte)) << 23);  // 2^(127 - byte), exact
+        uint32_t q = 0;
+        if (e8 != 255) {
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, raw[u].at(0) * inv, raw[u].at(1) * inv, 1.f, 0);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, raw[u].at(2) * inv, raw[u].at(3) * inv, 1.f, 1);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, raw[u].at(4) * inv, raw[u].at(5) * inv, 1.f, 2);
+          q = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(q, raw[u].at(6) * inv, raw[u].at(7) * inv, 1.f, 3);
+        }
+        if (c < a.H) {
+          *(uint32_t*)(a.codes + i * (a.H / 2) + c / 2) = q;
+          if (t % 4 == 0) a.scales[i * (a.H / kMxGroup) + c / kMxGroup] = (uint8_t)byte;
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int TPR>
+__global__ __launch_bounds__(256) void mxfp4_dequantize_kernel(const MxRowsArgs a) {
+  constexpr int kRows = 256 / TPR, kAhead = 2;
+  const int t = threadIdx.x % TPR;
+  for (int64_t i = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR; i < a.N; i += (int64_t)gridDim.x * kRows) {
+    for (int c0 = t * kNormVec; c0 < a.H; c0 += kAhead * TPR * kNormVec) {
+      uint32_t q[kAhead], byte[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int c = min(c0 + u * TPR * kNormVec, a.H - kNormVec);
+        q[u] = *(const uint32_t*)(a.codes + i * (a.H / 2) + c / 2);
+        byte[u] = a.scales[i * (a.H / kMxGroup) + c / kMxGroup];
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int c = c0 + u * TPR * kNormVec;
+        float y[kNormVec];
+#pragma unroll
+        for (int e = 0; e < kNormVec; ++e) {
+          const uint32_t m = (q[u] >> (4 * e)) & 7u;
+          // Twice the magnitude: 0, 1, 2, 3, 4, 6, 8, 12 (a byte each).
+          const float v = (float)((0x0c08060403020100ull >> (8 * m)) & 0xffu);
+          const float s = __builtin_amdgcn_ldexpf((q[u] >> (4 * e)) & 8u ? -v : v, (int)byte[u] - 128);
+          y[e] = byte[u] == 255 ? __builtin_nanf("") : s;
+        }
+        if (c < a.H) store_row<WHOLE>((T*)a.y + i * a.ld + c, kNormVec, y);
+      }
+    }
+  }
+}
+
+// ---- the product ----
+//
+// out[m][v] = sum_k x[m][k] w[v][k] with v_mfma_scale_f32_16x16x128_f8f6f4: a lane gives 32 values (16 bytes, one group, with
+// one scale byte) of row lane % 16. Any order of the groups serves as long as both operands have the same: of 256
+// values, lane quarter q takes groups 2q and 2q + 1 in turn, so that what it reads of a row is together.
+// W is the first operand: a lane then holds four consecutive v of one m.
+
+struct MxMatmulArgs {
+  const uint8_t *x, *x_scales, *w, *w_scales;
+  void* out;
+  int64_t out_ld;
+  int64_t M, V;
+  int K;
+  int tiles_m, tiles_v;
+};
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+template <int J>
+__device__ __forceinline__ f32x4 mx_mfma(const u32x4& w, uint32_t ws, const u32x4& x, uint32_t xs, f32x4 c) {
+  const i32x8 a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3]}, b = {(int)x[0], (int)x[1], (int)x[2], (int)x[3]};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, J, (int)ws, J, (int)xs);
+}
+
+// 256 values of K of a lane's row: two groups' codes and scale bytes.
+struct MxFragment {
+  u32x4 codes[2];
+  uint32_t scales;
+};
+constexpr int kMxStep = 256, kMxStepBytes = kMxStep / 2, kMxStepGroups = kMxStep / kMxGroup;
+constexpr uint32_t kMxOne = 0x7f7fu;  // two scales of 1
+
+__device__ __forceinline__ void mx_load(const uint8_t* codes, const uint8_t* scales, int step, MxFragment& f) {
+  __builtin_memcpy(&f.codes[0], codes + step * kMxStepBytes, 16);
+  __builtin_memcpy(&f.codes[1], codes + step * kMxStepBytes + 16, 16);
+  uint16_t s;
+  __builtin_memcpy(&s, scales + step * kMxStepGroups, 2);
+  f.scales = s;
+}
+// The last, shorter step: groups past the row's end are zeros.
+__device__ __forceinline__ void mx_load_tail(const uint8_t* codes, const uint8_t* scales, int step, int groups, int first, MxFragment& f) {
+  f.scales = 0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    f.codes[j] = (u32x4){};
+    uint32_t s = 127;
+    if (first + j < groups) {
+      __builtin_memcpy(&f.codes[j], codes + step * kMxStepBytes + 16 * j, 16);
+      s = scales[step * kMxStepGroups + j];
+    }
+    f.scales |= s << (8 * j);
+  }
+}
+
+// Few rows of x (up to 16 MT): W is read once, straight into registers, and nothing else takes long. A workgroup has 32 rows
+// of W; its four waves take the steps of K in turn, the next one requested under the current one's products, and add up at
+// the end. x comes from L2: 32 rows of W for each read of it.
+template <typename T, int MT>
+__global__ __launch_bounds__(256) void mxfp4_few_kernel(const MxMatmulArgs a) {
+  constexpr int kRowsW = 32, kPitch = kRowsW + 4, kWaves = 4;
+  __shared__ float sums[kWaves][16 * MT][kPitch];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
+  const int64_t v0 = (int64_t)blockIdx.x * kRowsW, pitch = a.K / 2, groups = a.K / kMxGroup;
+  const uint8_t *pw[2], *sw[2], *px[MT], *sx[MT];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int64_t v = min(v0 + 16 * i + row, a.V - 1);
+    pw[i] = a.w + v * pitch + 32 * quarter;
+    sw[i] = a.w_scales + v * groups + 2 * quarter;
+  }
+#pragma unroll
+  for (int j = 0; j < MT; ++j) {
+    const int64_t m = min((int64_t)16 * j + row, a.M - 1);
+    px[j] = a.x + m * pitch + 32 * quarter;
+    sx[j] = a.x_scales + m * groups + 2 * quarter;
+  }
+  f32x4 acc[2][MT] = {};
+  auto request = [&](int step, MxFragment (&w)[2], MxFragment (&x)[MT]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) mx_load(pw[i], sw[i], step, w[i]);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) mx_load(px[j], sx[j], step, x[j]);
+  };
+  auto multiply = [&](const MxFragment (&w)[2], const MxFragment (&x)[MT]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+        acc[i][j] = mx_mfma<0>(w[i].codes[0], w[i].scales, x[j].codes[0], x[j].scales, acc[i][j]);
+        acc[i][j] = mx_mfma<1>(w[i].codes[1], w[i].scales, x[j].codes[1], x[j].scales, acc[i][j]);
+      }
+  };
+  const int steps = a.K / kMxStep;
+  if (wave < steps) {
+    // (requests past the last step read it again: behind a branch the compiler would wait for all of them)
+    MxFragment w0[2], w1[2], x0[MT], x1[MT];
+    request(wave, w0, x0);
+    for (int s = wave;;) {
+      request(min(s + kWaves, steps - 1), w1, x1);
+      multiply(w0, x0);
+      if ((s += kWaves) >= steps) break;
+      request(min(s + kWaves, steps - 1), w0, x0);
+      multiply(w1, x1);
+      if ((s += kWaves) >= steps) break;
+    }
+  }
+  if (a.K % kMxStep != 0 && wave == steps % kWaves) {
+    MxFragment w[2], x[MT];
+    const int left = (a.K % kMxStep) / kMxGroup;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) mx_load_tail(pw[i], sw[i], steps, left, 2 * quarter, w[i]);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) mx_load_tail(px[j], sx[j], steps, left, 2 * quarter, x[j]);
+    multiply(w, x);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) *(f32x4*)&sums[wave][16 * j + row][16 * i + 4 * quarter] = acc[i][j];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < MT; k += 2) {
+    const int m = 16 * k + (int)threadIdx.x / 8, c = threadIdx.x % 8 * 4;
+    if (m >= 16 * MT || m >= a.M) break;
+    f32x4 y = *(f32x4*)&sums[0][m][c];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) y += *(f32x4*)&sums[w][m][c];
+    T* p = (T*)a.out + m * a.out_ld + v0 + c;
+    T q[4] = {from_f32<T>(y[0]), from_f32<T>(y[1]), from_f32<T>(y[2]), from_f32<T>(y[3])};
+    if (v0 + c + 4 <= a.V) {
+      __builtin_memcpy(p, q, sizeof(q));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v0 + c + e < a.V) p[e] = q[e];
+    }
+  }
+}
+
+// Many rows: a tile of 256 rows of W by BN of x for eight waves (4 x 2), each 64 by BN / 2 in 16 x 16 blocks. A step is 256
+// values of K, 128 bytes of a row: whole cache lines, LDS-DMA loads of 8 rows each into one of two slots. The 16-byte
+// pieces of LDS row r are permuted by r % 8, so that a fragment's 16 rows lie in distinct banks. The scales go through
+// registers, since their rows may begin at any byte.
+template <typename T, int BN>
+__global__ __launch_bounds__(512) void mxfp4_many_kernel(const MxMatmulArgs a) {
+  constexpr int kBM = 256, kI = 4, kJ = BN / 32, kWaves = 8;
+  constexpr int kW = kBM * kMxStepBytes, kX = BN * kMxStepBytes, kSw = kBM * kMxStepGroups, kSx = BN * kMxStepGroups;
+  constexpr int kSlot = kW + kX + kSw + kSx;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const uint32_t base = (uint32_t)(uintptr_t)(lds_void*)smem;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
+  int tm, tv;
+  tile_coords(blockIdx.x, gridDim.x, a.tiles_m, a.tiles_m, tm, tv);
+  const int64_t m0 = (int64_t)tm * BN, v0 = (int64_t)tv * kBM;
+  const uint32_t pitch = (uint32_t)a.K / 2, groups = (uint32_t)a.K / kMxGroup;
+  const int rows_w = (int)min(a.V - v0, (int64_t)kBM), rows_x = (int)min(a.M - m0, (int64_t)BN);
+  // Rows past the last are zeros by the descriptors' ranges.
+  const auto rsrc_w = make_rsrc((const void*)uniform64((uint64_t)(a.w + v0 * pitch)), __builtin_amdgcn_readfirstlane((uint32_t)rows_w * pitch));
+  const auto rsrc_x = make_rsrc((const void*)uniform64((uint64_t)(a.x + m0 * pitch)), __builtin_amdgcn_readfirstlane((uint32_t)rows_x * pitch));
+  const int steps = (a.K + kMxStep - 1) / kMxStep;
+  const uint32_t piece = (uint32_t)((lane & 7) ^ (lane >> 3)) * 16u, row_off = (uint32_t)(lane >> 3) * pitch;
+  auto dma = [&](int step, int slot) {
+    const uint32_t k = (uint32_t)step * kMxStepBytes;
+    // Pieces past the rows' end are zeros too.
+    const bool in = k + piece < pitch;
+    char* to = smem + slot * kSlot;
+#pragma unroll
+    for (int n = 0; n < kBM / 8 / kWaves; ++n) {
+      const int b = wave * (kBM / 8 / kWaves) + n;
+      dma16(rsrc_w, to + b * 1024, in ? row_off + piece + k + (uint32_t)(8 * b) * pitch : kOOB);
+    }
+#pragma unroll
+    for (int n = 0; n < BN / 8 / kWaves; ++n) {
+      const int b = wave * (BN / 8 / kWaves) + n;
+      dma16(rsrc_x, to + kW + b * 1024, in ? row_off + piece + k + (uint32_t)(8 * b) * pitch : kOOB);
+    }
+  };
+  // Thread t has the scales of W's row t, then of x's row t - 256.
+  const bool of_w = threadIdx.x < kBM;
+  const int srow = of_w ? min((int)threadIdx.x, rows_w - 1) : min((int)threadIdx.x - kBM, rows_x - 1);
+  const uint8_t* ps = of_w ? a.w_scales + (v0 + srow) * groups : a.x_scales + (m0 + srow) * groups;
+  const bool has_scales = threadIdx.x < kBM + BN;
+  auto load_scales = [&](int step) {
+    uint64_t s = 0x7f7f7f7f7f7f7f7full;
+    const uint32_t g = (uint32_t)step * kMxStepGroups;
+    if (!has_scales || step >= steps) return s;
+    if (g + kMxStepGroups <= groups) {
+      __builtin_memcpy(&s, ps + g, 8);
+    } else {
+      for (uint32_t k = g; k < groups; ++k) s = (s & ~(0xffull << (8 * (k - g)))) | (uint64_t)ps[k] << (8 * (k - g));
+    }
+    return s;
+  };
+  auto put_scales = [&](int slot, uint64_t s) {
+    if (has_scales) *(uint64_t*)(smem + slot * kSlot + kW + kX + threadIdx.x * 8) = s;
+  };
+  f32x4 acc[kI][kJ] = {};
+  const int wv = wave & 3, wm = wave >> 2;
+  // Fragment of block b (16 rows), group pair half j: piece 2 quarter + j of row 16 b + row.
+  const uint32_t frag0 = (uint32_t)(row * kMxStepBytes) + (uint32_t)(((2 * quarter) ^ (row & 7)) * 16);
+  const uint32_t addr_w = base + (uint32_t)(wv * 64 * kMxStepBytes) + frag0;
+  const uint32_t addr_x = base + kW + (uint32_t)(wm * (BN / 2) * kMxStepBytes) + frag0;
+  const uint32_t addr_sw = base + kW + kX + (uint32_t)((wv * 64 + row) * kMxStepGroups + 2 * quarter);
+  const uint32_t addr_sx = base + kW + kX + kSw + (uint32_t)((wm * (BN / 2) + row) * kMxStepGroups + 2 * quarter);
+  dma(0, 0);
+  put_scales(0, load_scales(0));
+  uint64_t next = load_scales(1);
+  for (int t = 0; t < steps; ++t) {
+    const uint32_t slot = (uint32_t)(t & 1) * kSlot;
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (t + 1 < steps) {
+      dma(t + 1, (t + 1) & 1);
+      put_scales((t + 1) & 1, next);
+      next = load_scales(t + 2);
+    }
+    uint32_t sw[kI], sx[kJ];
+#pragma unroll
+    for (int i = 0; i < kI; ++i) sw[i] = *lds_at<uint16_t>(addr_sw + slot + i * 16 * kMxStepGroups);
+#pragma unroll
+    for (int j = 0; j < kJ; ++j) sx[j] = *lds_at<uint16_t>(addr_sx + slot + j * 16 * kMxStepGroups);
+    auto half = [&](auto h) {
+      constexpr int kH = decltype(h)::value;
+      u32x4 w[kI], x[kJ];
+      // (the pieces' permutation flips bits 4 to 6; group 2 quarter + 1 is group 2 quarter's bit 4 flipped)
+#pragma unroll
+      for (int i = 0; i < kI; ++i) w[i] = *lds_at<u32x4>(((addr_w + slot) ^ (16u * kH)) + i * 16 * kMxStepBytes);
+#pragma unroll
+      for (int j = 0; j < kJ; ++j) x[j] = *lds_at<u32x4>(((addr_x + slot) ^ (16u * kH)) + j * 16 * kMxStepBytes);
+#pragma unroll
+      for (int j = 0; j < kJ; ++j)
+#pragma unroll
+        for (int i = 0; i < kI; ++i) acc[i][j] = mx_mfma<kH>(w[i], sw[i], x[j], sx[j], acc[i][j]);
+    };
+    half(std::integral_constant<int, 0>{});
+    half(std::integral_constant<int, 1>{});
+  }
+  // Element r of block (i, j): v = 16 i + 4 quarter + r, m = 16 j + row of the wave's part.
+#pragma unroll
+  for (int j = 0; j < kJ; ++j) {
+    const int64_t m = m0 + wm * (BN / 2) + 16 * j + row;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int i = 0; i < kI; i += 2) {
+        const int64_t v = v0 + wv * 64 + 16 * i + 8 * quarter;
+        const u32x4 y = regroup16<T>(acc[i][j], acc[i + 1][j]);
+        T* p = (T*)a.out + m * a.out_ld + v;
+        if (m >= a.M) continue;
+        if (v + 8 <= a.V) {
+          __builtin_memcpy(p, &y, 16);
+        } else {
+          T q[8];
+          __builtin_memcpy(q, &y, 16);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (v + e < a.V) p[e] = q[e];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kI; ++i) {
+        const int64_t v = v0 + wv * 64 + 16 * i + 4 * quarter;
+        T* p = (T*)a.out + m * a.out_ld + v;
+        if (m >= a.M) continue;
+        if (v + 4 <= a.V) {
+          __builtin_memcpy(p, &acc[i][j], 16);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (v + e < a.V) p[e] = acc[i][j][e];
+        }
+      }
+    }
+  }
+}
+template <int BN>
+constexpr int mx_many_smem() { return 2 * (256 + BN) * (kMxStepBytes + kMxStepGroups); }
+
+}  // namespace lce

@@ -15,7 +15,8 @@ from . import ops
 from .lce import DTYPES, LCEError, load_library
 from .ops import _check_unfollowed, _pitch, _space, _upstream, _written
 
-EXPORTED = ("lce_embedding_forward", "lce_embedding_workspace_size", "lce_embedding_backward")
+EXPORTED = ("lce_embedding_forward", "lce_embedding_workspace_size", "lce_embedding_backward", "lce_mxfp4_quantize",
+            "lce_mxfp4_dequantize", "lce_mxfp4_matmul")
 _TOKENS = {torch.int64: 8, torch.int32: 4}
 
 _lib = None
@@ -30,7 +31,10 @@ def _library() -> ctypes.CDLL:
     for name, args, res in [
             ("lce_embedding_forward", [vp, ci, i64, vp, i64, i64, i64, ci, f32, vp, i64, vp], ci),
             ("lce_embedding_workspace_size", [i64, i64], sz),
-            ("lce_embedding_backward", [vp, i64, vp, ci, i64, i64, i64, ci, f32, i64, vp, i64, ci, vp, sz, vp], ci)]:
+            ("lce_embedding_backward", [vp, i64, vp, ci, i64, i64, i64, ci, f32, i64, vp, i64, ci, vp, sz, vp], ci),
+            ("lce_mxfp4_quantize", [vp, i64, i64, i64, ci, vp, vp, vp], ci),
+            ("lce_mxfp4_dequantize", [vp, vp, i64, i64, ci, vp, i64, vp], ci),
+            ("lce_mxfp4_matmul", [vp, vp, i64, vp, vp, i64, i64, ci, vp, i64, vp], ci)]:
         f = getattr(lib, name)
         f.argtypes, f.restype = args, res
     _lib = lib
@@ -172,3 +176,84 @@ class Embedding(torch.autograd.Function):
 def embedding(tokens, weight, scale: float = 1.0, padding_idx: int | None = None):
     """scale * weight[tokens]. Differentiable (once) with respect to weight; rows of padding_idx get no gradient."""
     return Embedding.apply(tokens, weight, scale, padding_idx)
+
+
+# ---- rows and weights in 4 bits --------------------------------------------------------------------
+
+MXFP4_GROUP = 32
+
+
+def _check_codes(codes, scales, what: str):
+    """The leading shape and H of a matrix in 4 bits."""
+    if not codes.is_cuda or codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or scales.device != codes.device:
+        raise ValueError(f"{what}: codes and scales must be uint8 tensors of one device")
+    H = 2 * codes.shape[-1] if codes.dim() else 0
+    if H < MXFP4_GROUP or H % MXFP4_GROUP or scales.shape != codes.shape[:-1] + (H // MXFP4_GROUP,):
+        raise ValueError(f"{what}: codes must be [..., H/2] and scales [..., H/32], H a multiple of 32")
+    if not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError(f"{what}: codes and scales must be contiguous")
+    return codes.shape[:-1], H
+
+
+def mxfp4_quantize(hidden, codes=None, scales=None):
+    """(codes, scales): rows [..., H] (H a multiple of 32) in 4 bits with a power of two for each 32 values (OCP MXFP4).
+
+    codes [..., H/2] (uint8) hold two values a byte, the first in the low half: sign, two bits of exponent, one of mantissa
+    (0, 0.5, 1, 1.5, 2, 3, 4, 6). scales [..., H/32] (uint8) hold exponents + 127: that of the group's largest magnitude less 2.
+    A group with a NaN or an infinity has scale 255. Both may be given. Not differentiable.
+    """
+    dev = _device_rows(hidden, "hidden")
+    H = hidden.shape[-1] if hidden.dim() else 0
+    if H < MXFP4_GROUP or H % MXFP4_GROUP:
+        raise ValueError("hidden must be [..., H] with H a multiple of 32")
+    pitch, lead = _pitch(hidden, "hidden"), hidden.shape[:-1]
+    outs = []
+    for t, n, what in ((codes, H // 2, "codes"), (scales, H // MXFP4_GROUP, "scales")):
+        if t is None:
+            t = hidden.new_empty(lead + (n,), dtype=torch.uint8)
+        elif not _given(t, lead + (n,), torch.uint8, dev, what).is_contiguous():
+            raise ValueError(f"{what} must be contiguous")
+        outs.append(t)
+    codes, scales = outs
+    _call("lce_mxfp4_quantize", dev, hidden.data_ptr(), pitch, hidden.numel() // H, H, DTYPES[hidden.dtype], codes.data_ptr(), scales.data_ptr())
+    return codes, scales
+
+
+def mxfp4_dequantize(codes, scales, dtype=torch.bfloat16, out=None):
+    """The values [..., H] that codes and scales stand for, rounded once to dtype. Not differentiable."""
+    lead, H = _check_codes(codes, scales, "mxfp4")
+    if dtype not in DTYPES:
+        raise ValueError("dtype must be bfloat16, float16 or float32")
+    if out is None:
+        out, pitch = codes.new_empty(lead + (H,), dtype=dtype), H
+    else:
+        pitch = _pitch(_given(out, lead + (H,), dtype, codes.device, "out"), "out")
+    _call("lce_mxfp4_dequantize", codes.device, codes.data_ptr(), scales.data_ptr(), out.numel() // H, H, DTYPES[dtype], out.data_ptr(), pitch)
+    return out
+
+
+def mxfp4_matmul(codes, scales, weight_codes, weight_scales, dtype=torch.bfloat16, out=None):
+    """Rows [..., H] times a weight [V, H], both in 4 bits: [..., V] in dtype, summed in fp32, rounded once. Not differentiable."""
+    lead, H = _check_codes(codes, scales, "rows")
+    shape, weight_H = _check_codes(weight_codes, weight_scales, "weight")
+    if len(shape) != 1 or weight_H != H or weight_codes.device != codes.device:
+        raise ValueError("the weight must be [V, H] with the rows' H, on their device")
+    if dtype not in DTYPES:
+        raise ValueError("dtype must be bfloat16, float16 or float32")
+    V = shape[0]
+    if out is None:
+        out, pitch = codes.new_empty(lead + (V,), dtype=dtype), V
+    else:
+        pitch = _pitch(_given(out, lead + (V,), dtype, codes.device, "out"), "out")
+    _call("lce_mxfp4_matmul", codes.device, codes.data_ptr(), scales.data_ptr(), lead.numel(), weight_codes.data_ptr(), weight_scales.data_ptr(),
+          V, H, DTYPES[dtype], out.data_ptr(), pitch)
+    return out
+
+
+def mxfp4_linear(hidden, weight_codes, weight_scales, out=None):
+    """hidden [..., H], quantised here, times a weight in 4 bits: [..., V] of hidden's type (an output layer's logits).
+
+    Not differentiable: training keeps the weight in its own type (linear_cross_entropy).
+    """
+    codes, scales = mxfp4_quantize(hidden)
+    return mxfp4_matmul(codes, scales, weight_codes, weight_scales, hidden.dtype, out)
