@@ -72,6 +72,40 @@ lce_status_t lce_mxfp4_dequantize(const void* codes, const void* scales, int64_t
 lce_status_t lce_mxfp4_matmul(const void* x_codes, const void* x_scales, int64_t M, const void* w_codes, const void* w_scales,
                               int64_t V, int64_t H, int dtype, void* out, int64_t out_ld, void* stream);
 
+/*
+ * A token for each row of logits z. With m the row's largest logit and w_v = exp((z_v - m) / temperature), in the order of falling
+ * z, equal ones by rising v:
+ *   top_k  keeps the first top_k (0 or at least V: all),
+ *   top_p  of these, the ones whose predecessors weigh less than top_p of these together (1 or more: all; the first always),
+ *   min_p  of these, the ones with w_v >= min_p (0 or less: all; 1 at most).
+ * token = the first kept v for which the sum of kept w up to and with v, by rising v, is above u times the sum of all kept.
+ * A temperature that is not above 0 takes the largest logit's first place. A row with a NaN, or nothing above -inf, or whose u is NaN, gives
+ * -1; u below 0 counts as 0, from 1 on the last kept token comes. +inf are the largest and equal. Weights are computed in 64 bits and
+ * added in integers (a 2^42nd of the largest weight, or less): a token's smaller weight counts as none, and a result does
+ * not depend on the order of additions.
+ *   logits      : device [N,V] of dtype, 1 <= V <= LCE_SAMPLE_MAX_V, N <= LCE_SAMPLE_MAX_N; only read.
+ *   uniforms    : device fp32 [N], the random numbers u.
+ *   settings    : in HOST memory, read during the call: one value for all rows, or, where the pointer is not NULL, device [N] with
+ *                 each row's.
+ *   tokens      : device int64 [N].
+ *   logprobs    : device fp32 [N], the log of token's share of the kept weights (0 for a temperature not above 0, NaN with token -1);
+ *                 NULL where it is not wanted.
+ *   workspace   : device memory of lce_sample_workspace_size(N, V) bytes, 256-byte aligned. The size does not fall as N grows. Calls
+ *                 (and captured graphs) that may run at the same time need one each.
+ */
+#define LCE_SAMPLE_MAX_V (1 << 20)
+#define LCE_SAMPLE_MAX_N (1 << 16)
+typedef struct {
+  float temperature, top_p, min_p;
+  int32_t top_k;
+  const float *temperatures, *top_ps, *min_ps;
+  const int32_t* top_ks;
+} lce_sample_t;
+size_t lce_sample_workspace_size(int64_t N, int64_t V);
+lce_status_t lce_sample(const void* logits, int64_t logits_ld, int64_t N, int64_t V, int dtype, const float* uniforms,
+                        const lce_sample_t* settings, int64_t* tokens, float* logprobs, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

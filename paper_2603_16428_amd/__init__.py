@@ -9,7 +9,7 @@ from .ops import (AddRMSNorm, add_rmsnorm, add_rmsnorm_backward, add_rmsnorm_for
                   add_rmsnorm_workspace_size, clip_grad_norm, clip_grad_norm_, grad_norm, grad_norm_workspace_size,
                   rmsnorm)
 from .vocab import (Embedding, embedding, embedding_backward, embedding_forward, embedding_workspace_size, mxfp4_dequantize,
-                    mxfp4_linear, mxfp4_matmul, mxfp4_quantize)
+                    mxfp4_linear, mxfp4_matmul, mxfp4_quantize, sample, sample_workspace_size)
 
 __all__ = ["AdamConfig", "AddRMSNorm", "HeadState", "HeadStepTiming", "LCEError", "LinearCrossEntropy", "Embedding", "PlanInfo",
            "RMSNormLinearCrossEntropy", "add_rmsnorm", "add_rmsnorm_backward", "add_rmsnorm_forward",
@@ -19,5 +19,6 @@ __all__ = ["AdamConfig", "AddRMSNorm", "HeadState", "HeadStepTiming", "LCEError"
            "head_train_step",
            "host_adam_step", "linear_cross_entropy", "load_library", "mxfp4_dequantize", "mxfp4_linear", "mxfp4_matmul",
            "mxfp4_quantize", "plan_info", "rmsnorm", "rmsnorm_forward",
-           "rmsnorm_forward_backward", "rmsnorm_linear_cross_entropy", "rmsnorm_workspace_size", "timing_enable",
+           "rmsnorm_forward_backward", "rmsnorm_linear_cross_entropy", "rmsnorm_workspace_size", "sample",
+           "sample_workspace_size", "timing_enable",
            "timing_read", "workspace_size"]

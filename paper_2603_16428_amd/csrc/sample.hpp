@@ -1,0 +1,541 @@
+// A token for each row of logits, from a given random number: temperature, top-k, top-p, min-p.
+//
+// Weights exp((z - max) / T) are computed in 64 bits and added as 64-bit integers (fixed point: 2^-44 of the largest weight for
+// a vocabulary of 2^18, and more for smaller ones). Integer sums do not depend on their order, so counts and weights are gathered by
+// LDS atomics, and everything that is looked for (the k-th largest, where top-p ends, which of several equal ones are still in,
+// the token whose running sum passes u Z) is found the same way: 2048 bins over the range in question, a prefix sum, the bin
+// where the target is reached, and again inside that bin until it is one value. Nothing is sorted.
+//
+// Two launches: parts of a row in parallel (the maximum of each group of 64 logits, sums of weights where the whole row's
+// is needed), then a workgroup per row. Its settings and the groups' maxima give a bound that no kept logit is below: only
+// groups above it are read again, and, where few logits pass, they are listed in LDS.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ops_row.hpp"
+
+namespace lce {
+
+constexpr int kSampleParts = 64, kPartGroups = 64, kMostGroups = kSampleParts * kPartGroups;
+
+struct SampleArgs {
+  const void* logits;
+  int64_t ld;  // elements
+  const float* u;
+  float temperature, top_p, min_p;
+  int top_k;
+  const float *temperatures, *top_ps, *min_ps;  // of each row, or null
+  const int32_t* top_ks;
+  int64_t* tokens;
+  float* logprobs;
+  float *group_max, *part_max;  // [N][groups], [N][parts]
+  double* part_sum;             // [N][parts], relative to the part's maximum
+  int V, groups, parts, bits;   // bits: a weight of 1 is 2^bits
+};
+
+struct SampleRow {
+  double rate;  // 256 log2(e) / T
+  float T, p, least;
+  int k;  // 0: all
+  bool greedy, by_k, by_p, by_least;
+  __device__ __forceinline__ bool whole() const { return !by_k && !by_p && !by_least; }
+  // Whether the sum of the whole row's weights is needed.
+  __device__ __forceinline__ bool sums() const { return !greedy && !by_k && (by_p || whole()); }
+};
+__device__ __forceinline__ SampleRow sample_row(const SampleArgs& a, int64_t i) {
+  SampleRow r;
+  r.T = a.temperatures ? a.temperatures[i] : a.temperature;
+  r.p = a.top_ps ? a.top_ps[i] : a.top_p;
+  r.least = fminf(a.min_ps ? a.min_ps[i] : a.min_p, 1.f);  // the largest is always kept
+  r.k = a.top_ks ? a.top_ks[i] : a.top_k;
+  r.greedy = !(r.T > 0.f);
+  r.by_k = r.k > 0 && r.k < a.V;
+  r.by_p = r.p < 1.f;
+  r.by_least = r.least > 0.f;
+  r.rate = 256.0 * 1.4426950408889634074 / (double)r.T;
+  return r;
+}
+
+// exp from its argument times 256 log2(e): 2^(n / 256) from a table and the rest's series, whose next term is below 4e-17.
+// (Far below the smallest weight that counts, so that infinities pass.)
+__device__ __forceinline__ double sample_exp(double t, const double* table) {
+  constexpr double c1 = 0.69314718055994530942 / 256, c2 = c1 * c1 / 2, c3 = c1 * c1 * c1 / 6, c4 = c1 * c1 * c1 * c1 / 24;
+  t = fmax(t, -65536.0);
+  const double n = rint(t), f = t - n;
+  const int i = (int)n;
+  return __builtin_ldexp(table[i & 255] * fma(f, fma(f, fma(f, fma(f, c4, c3), c2), c1), 1.0), i >> 8);
+}
+__device__ __forceinline__ void sample_table(double* table) {
+  if (threadIdx.x < 256) table[threadIdx.x] = exp2((double)threadIdx.x / 256.0);
+}
+// The weight of z relative to `top`, 1 where they are equal (infinities too).
+__device__ __forceinline__ double sample_weight(float z, float top, double rate, const double* table) {
+  const double w = sample_exp(((double)z - (double)top) * rate, table);
+  return z == top ? 1.0 : w;
+}
+
+// The larger of two, and NaN if one is.
+__device__ __forceinline__ float max_or_nan(float a, float b) { return (a >= b || a != a) ? a : b; }
+
+// A workgroup for each part (64 groups): eight lanes a group, REP pieces of 8 logits each.
+template <typename T, int REP, RowEnd END>
+__global__ __launch_bounds__(256) void sample_parts_kernel(const SampleArgs a) {
+  constexpr int kGroup = 64 * REP, kRounds = kPartGroups / 32;
+  __shared__ double table[256], sums[4];
+  __shared__ float tops[4];
+  const int64_t i = blockIdx.x / a.parts;
+  const int part = blockIdx.x % a.parts;
+  const T* row = (const T*)a.logits + i * a.ld;
+  const SampleRow set = sample_row(a, i);
+  const bool summed = set.sums();
+  RawRow<T> raw[kRounds][REP];
+#pragma unroll
+  for (int g = 0; g < kRounds; ++g)
+#pragma unroll
+    for (int r = 0; r < REP; ++r) {
+      const int at = (part * kPartGroups + g * 32 + (int)threadIdx.x / 8) * kGroup + r * 64 + (threadIdx.x % 8) * kNormVec;
+      raw[g][r].clear();
+      load_raw<END>(row + at, a.V - at, raw[g][r]);
+    }
+  if (summed) sample_table(table);
+  float top = -INFINITY;
+  auto count_of = [&](int g, int r) {  // logits of this piece
+    return a.V - ((part * kPartGroups + g * 32 + (int)threadIdx.x / 8) * kGroup + r * 64 + ((int)threadIdx.x % 8) * kNormVec);
+  };
+#pragma unroll
+  for (int g = 0; g < kRounds; ++g) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < REP; ++r) {
+      const int n = count_of(g, r);
+      align_end<END>(n, raw[g][r]);
+#pragma unroll
+      for (int e = 0; e < kNormVec; ++e) m = e < n ? max_or_nan(raw[g][r].at(e), m) : m;
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) m = max_or_nan(__shfl_xor(m, o), m);
+    const int group = part * kPartGroups + g * 32 + (int)threadIdx.x / 8;
+    if (threadIdx.x % 8 == 0 && group < a.groups) a.group_max[i * a.groups + group] = m;
+    top = max_or_nan(m, top);
+  }
+  if (!summed) return;
+#pragma unroll
+  for (int o = 8; o < 64; o <<= 1) top = max_or_nan(__shfl_xor(top, o), top);
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = max_or_nan(max_or_nan(tops[0], tops[1]), max_or_nan(tops[2], tops[3]));
+  double sum = 0.0;
+  if (top > -INFINITY) {
+#pragma unroll
+    for (int g = 0; g < kRounds; ++g)
+#pragma unroll
+      for (int r = 0; r < REP; ++r)
+#pragma unroll
+        for (int e = 0; e < kNormVec; ++e)
+          if (e < count_of(g, r)) sum += sample_weight(raw[g][r].at(e), top, set.rate, table);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.part_max[i * a.parts + part] = top;
+    a.part_sum[i * a.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  }
+}
+
+// ---- a row's token ----
+
+// An order of the logits by integers, and back. 16-bit types use the bits that they have.
+template <typename T>
+struct SampleKey {
+  static constexpr int kShift = sizeof(T) == 4 ? 0 : std::is_same_v<T, bf16> ? 16 : 13;
+  static __device__ __forceinline__ uint32_t of(float z) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, z + 0.f);  // (-0 is 0)
+    return (b >> 31 ? ~b : b | 0x80000000u) >> kShift;
+  }
+  static __device__ __forceinline__ float value(uint32_t key) {
+    const uint32_t b = key << kShift;
+    return __builtin_bit_cast(float, b >> 31 ? b & 0x7fffffffu : ~(b | ((1u << kShift) - 1u)));
+  }
+};
+
+constexpr int kSampleThreads = 1024, kSampleBins = 2 * kSampleThreads, kSampleList = 4096;
+
+struct SampleFound {
+  int bin;  // -1: the target is not reached
+  uint32_t before, count, all;
+  uint64_t weight_before, weight, weight_all;
+};
+struct SampleLds {
+  double table[256];
+  unsigned long long weight[kSampleBins];
+  uint32_t count[kSampleBins];
+  uint32_t list_key[kSampleList], list_at[kSampleList];
+  uint16_t active[kMostGroups];
+  uint64_t wave_weight[16];
+  uint32_t wave_count[16];
+  float wave_max[16];
+  uint32_t actives, listed, lowest;
+  SampleFound found;
+};
+
+__device__ __forceinline__ void sample_clear(SampleLds& s) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    s.weight[threadIdx.x + k * kSampleThreads] = 0;
+    s.count[threadIdx.x + k * kSampleThreads] = 0;
+  }
+  __syncthreads();
+}
+
+// The first bin with which the counts reach `count` or the weights `weight` (u >= 0: the first whose running weight is above u
+// times the whole). All threads, after their additions to the bins.
+__device__ __forceinline__ SampleFound sample_find(SampleLds& s, uint32_t count, uint64_t weight, double u = -1.0) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = 2 * threadIdx.x;
+  __syncthreads();
+  if (threadIdx.x == 0) s.found.bin = -1;
+  const uint32_t c0 = s.count[b], c1 = s.count[b + 1];
+  const uint64_t w0 = s.weight[b], w1 = s.weight[b + 1];
+  uint32_t c = c0 + c1;
+  uint64_t w = w0 + w1;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t cb = __shfl_up(c, o);
+    const uint64_t wb = __shfl_up((unsigned long long)w, o);
+    if (lane >= o) {
+      c += cb;
+      w += wb;
+    }
+  }
+  if (lane == 63) {
+    s.wave_count[wave] = c;
+    s.wave_weight[wave] = w;
+  }
+  __syncthreads();
+  uint32_t all_c = 0;
+  uint64_t all_w = 0;
+#pragma unroll
+  for (int k = 0; k < kSampleThreads / 64; ++k) {
+    if (k == wave) {
+      c += all_c;
+      w += all_w;
+    }
+    all_c += s.wave_count[k];
+    all_w += s.wave_weight[k];
+  }
+  if (u >= 0.0) {
+    weight = (uint64_t)(fmin(u, 1.0) * (double)all_w) + 1;
+    weight = weight > all_w ? all_w : weight;
+  }
+  c -= c0 + c1;
+  w -= w0 + w1;
+  auto reached = [&](uint32_t cc, uint64_t ww) { return cc >= count || ww >= weight; };
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t ck = k ? c1 : c0;
+    const uint64_t wk = k ? w1 : w0;
+    if (!reached(c, w) && reached(c + ck, w + wk)) s.found = {b + k, c, ck, all_c, w, wk, all_w};
+    c += ck;
+    w += wk;
+  }
+  __syncthreads();
+  SampleFound f = s.found;
+  f.all = all_c;
+  f.weight_all = all_w;
+  return f;
+}
+
+__device__ __forceinline__ float sample_block_max(float v, SampleLds& s) {
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) v = max_or_nan(__shfl_xor(v, o), v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s.wave_max[threadIdx.x >> 6] = v;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kSampleThreads / 64; ++k) v = max_or_nan(s.wave_max[k], v);
+  return v;
+}
+
+// Bits by which a span of values is shifted to fall into the bins.
+__device__ __forceinline__ int sample_shift(uint32_t span) { return span < (uint32_t)kSampleBins ? 0 : 21 - __builtin_clz(span); }
+static_assert(kSampleBins == 1 << 11, "sample_shift");
+
+template <typename T, int REP, RowEnd END>
+__global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const SampleArgs a) {
+  using Key = SampleKey<T>;
+  constexpr int kGroup = 64 * REP, kEach = kMostGroups / kSampleThreads;
+  __shared__ SampleLds s;
+  const int tid = threadIdx.x;
+  const int64_t i = blockIdx.x;
+  const T* row = (const T*)a.logits + i * a.ld;
+  const SampleRow set = sample_row(a, i);
+  const float u = a.u[i];
+  float maxima[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int g = tid + k * kSampleThreads;
+    maxima[k] = g < a.groups ? a.group_max[i * a.groups + g] : -INFINITY;
+  }
+  sample_table(s.table);
+  if (tid == 0) {
+    s.actives = s.listed = 0;
+    s.lowest = ~0u;
+  }
+  float top = maxima[0];
+#pragma unroll
+  for (int k = 1; k < kEach; ++k) top = max_or_nan(maxima[k], top);
+  top = sample_block_max(top, s);
+  auto answer = [&](int64_t token, float logprob) {
+    if (tid == 0) {
+      a.tokens[i] = token;
+      if (a.logprobs != nullptr) a.logprobs[i] = logprob;
+    }
+  };
+  // A NaN among the logits or for u, or nothing above -inf.
+  if (!(top > -INFINITY) || u != u) return answer(-1, __builtin_nanf(""));
+
+  // The logits of a range of places, by single loads.
+  auto range = [&](uint32_t lo, uint32_t n, auto f) {
+    for (uint32_t k = tid; k < n; k += kSampleThreads)
+      if (lo + k < (uint32_t)a.V) {
+        const float z = to_f32(row[lo + k]);
+        f(Key::of(z), z, lo + k);
+      }
+  };
+
+  if (set.greedy) {
+    uint32_t g0 = ~0u;
+#pragma unroll
+    for (int k = kEach - 1; k >= 0; --k)
+      if (maxima[k] == top) g0 = tid + k * kSampleThreads;
+    if (g0 != ~0u) atomicMin(&s.lowest, g0);
+    __syncthreads();
+    g0 = s.lowest;
+    __syncthreads();
+    if (tid == 0) s.lowest = ~0u;
+    __syncthreads();
+    range(g0 * kGroup, kGroup, [&](uint32_t, float z, uint32_t at) {
+      if (z == top) atomicMin(&s.lowest, at);
+    });
+    __syncthreads();
+    return answer(s.lowest, 0.f);
+  }
+
+  const double one = __builtin_ldexp(1.0, a.bits);
+  // A weight in fixed point: below 2^52, so that adding 2^52 rounds it to an integer in the low bits.
+  auto fixed = [&](double w) { return __builtin_bit_cast(uint64_t, fma(w, one, 0x1p52)) - __builtin_bit_cast(uint64_t, 0x1p52); };
+  // The token whose running sum of `weight_of` (key, logit, place) passes u times the whole, of places lo .. lo + n - 1, which
+  // `each` goes through. Its place, and the whole.
+  auto draw = [&](uint32_t lo, uint32_t n, double part, auto each, auto weight_of, uint64_t& whole) {
+    uint64_t target = 0;
+    for (bool first = true;; first = false) {
+      const int shift = sample_shift(n - 1);
+      sample_clear(s);
+      auto add = [&](uint32_t key, float z, uint32_t at) {
+        if (at - lo >= n) return;
+        const uint64_t w = weight_of(key, z, at);
+        if (w != 0) atomicAdd(&s.weight[(at - lo) >> shift], (unsigned long long)w);
+      };
+      if (first) each(add);
+      else if (n <= (uint32_t)kGroup * kPartGroups) range(lo, n, add);
+      else each(add);
+      const SampleFound f = first ? sample_find(s, ~0u, 0, part) : sample_find(s, ~0u, target);
+      if (first) {
+        whole = f.weight_all;
+        target = (uint64_t)(fmin(part, 1.0) * (double)whole) + 1;
+        target = target > whole ? whole : target;
+      }
+      if (f.bin < 0) return lo;  // (no weight at all, which the kept ones' largest rules out)
+      target -= f.weight_before;
+      lo += (uint32_t)f.bin << shift;
+      n = min(n - ((uint32_t)f.bin << shift), 1u << shift);
+      if (shift == 0) return lo;
+    }
+  };
+  auto logprob = [&](uint32_t at, double sum) {
+    const float z = to_f32(row[at]);
+    return (float)((z == top ? 0.0 : ((double)z - (double)top) / (double)set.T) - log(sum));
+  };
+  const double chance = u > 0.f ? (double)u : 0.0;
+
+  // The whole row's weight from its parts'.
+  double sum = 0.0;
+  if (set.sums()) {
+    sample_clear(s);
+    if (tid < a.parts) {
+      const double w = a.part_sum[i * a.parts + tid] * sample_weight(a.part_max[i * a.parts + tid], top, set.rate, s.table);
+      s.weight[tid] = (uint64_t)(w * one + 0.5);
+    }
+    const SampleFound f = sample_find(s, ~0u, 0, chance);
+    sum = (double)f.weight_all / one;
+    if (set.whole()) {
+      // Inside the part, relative to its own maximum.
+      const float of = a.part_max[i * a.parts + f.bin];
+      const double inside = (fmin(chance, 1.0) * (double)f.weight_all - (double)f.weight_before) / (double)f.weight;
+      const uint32_t lo = (uint32_t)f.bin * kPartGroups * kGroup, n = min((uint32_t)(kPartGroups * kGroup), (uint32_t)a.V - lo);
+      uint64_t whole;
+      const uint32_t at = draw(lo, n, fmin(fmax(inside, 0.0), 1.0), [&](auto add) { range(lo, n, add); },
+                               [&](uint32_t, float z, uint32_t) { return fixed(sample_weight(z, of, set.rate, s.table)); }, whole);
+      return answer(at, logprob(at, sum));
+    }
+  }
+
+  // No kept logit is below `bound`.
+  float bound = -INFINITY;
+  if (set.by_k && set.k <= a.groups && top < INFINITY) {
+    // The k-th largest of the groups' maxima: k logits at least are as large.
+    float least = INFINITY;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (maxima[k] > -INFINITY) least = fminf(least, maxima[k]);
+    least = -sample_block_max(-least, s);
+    const float inv = top > least ? (float)(kSampleBins - 1) / (top - least) : 0.f;
+    if (inv < INFINITY && top - least < INFINITY) {
+      auto bin = [&](float m) { return min((int)((top - m) * inv), kSampleBins - 1); };
+      sample_clear(s);
+#pragma unroll
+      for (int k = 0; k < kEach; ++k)
+        if (maxima[k] > -INFINITY) atomicAdd(&s.count[bin(maxima[k])], 1u);
+      const SampleFound f = sample_find(s, (uint32_t)set.k, ~0ull);
+      if (f.bin >= 0) {
+        float lowest = INFINITY;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+          if (maxima[k] > -INFINITY && bin(maxima[k]) <= f.bin) lowest = fminf(lowest, maxima[k]);
+        bound = -sample_block_max(-lowest, s);
+      }
+    }
+  }
+  // Those of a weight below w: (with room for the rounding of this bound)
+  auto bound_of = [&](double w) {
+    const double b = (double)top + (double)set.T * log(w);
+    return (float)(b - 1e-6 * fabs(b) - 1e-6 * (double)set.T);
+  };
+  if (set.by_least && !(set.by_k && set.by_p)) bound = fmaxf(bound, bound_of((double)set.least));
+  // Those below (1 - p) Z / V together weigh less than (1 - p) Z.
+  if (set.by_p && set.p <= 0.f) bound = top;
+  else if (set.by_p && !set.by_k) bound = fmaxf(bound, bound_of((1.0 - (double)set.p) * sum / (double)a.V));
+
+#pragma unroll
+  for (int k = 0; k < kEach; ++k)
+    if (maxima[k] >= bound && tid + k * kSampleThreads < a.groups) s.active[atomicAdd(&s.actives, 1u)] = (uint16_t)(tid + k * kSampleThreads);
+  __syncthreads();
+  const int actives = (int)s.actives;
+  // The logits of the active groups that are not below the bound: eight lanes a group, four groups requested at once.
+  auto stream = [&](auto f) {
+    constexpr int kAhead = 4, kAtOnce = kSampleThreads / 8;
+    for (int k0 = tid / 8; k0 < actives; k0 += kAhead * kAtOnce) {
+#pragma unroll
+      for (int r = 0; r < REP; ++r) {
+        RawRow<T> raw[kAhead];
+        int at[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+          at[q] = (int)s.active[min(k0 + q * kAtOnce, actives - 1)] * kGroup + r * 64 + (tid % 8) * kNormVec;
+          raw[q].clear();
+          load_raw<END>(row + at[q], a.V - at[q], raw[q]);
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+          const int n = k0 + q * kAtOnce < actives ? a.V - at[q] : 0;
+          align_end<END>(a.V - at[q], raw[q]);
+#pragma unroll
+          for (int e = 0; e < kNormVec; ++e) {
+            const float z = raw[q].at(e);
+            if (e < n && z >= bound) f(Key::of(z), z, (uint32_t)(at[q] + e));
+          }
+        }
+      }
+    }
+  };
+  stream([&](uint32_t key, float, uint32_t at) {
+    const uint32_t k = atomicAdd(&s.listed, 1u);
+    if (k < (uint32_t)kSampleList) {
+      s.list_key[k] = key;
+      s.list_at[k] = at;
+    }
+  });
+  __syncthreads();
+  const uint32_t listed = s.listed;
+  auto each = [&](auto f) {
+    if (listed <= (uint32_t)kSampleList) {
+      for (uint32_t k = tid; k < listed; k += kSampleThreads) f(s.list_key[k], Key::value(s.list_key[k]), s.list_at[k]);
+    } else {
+      stream(f);
+    }
+  };
+  auto weight = [&](float z) { return sample_weight(z, top, set.rate, s.table); };
+
+  // Falling logits, equal ones by their places: place and key in one number. Kept are those from `cut` on.
+  auto rank = [](uint32_t key, uint32_t at) { return (uint64_t)key << 32 | (0xffffffffu - at); };
+  uint64_t cut = 0;
+  // Makes the cut at the smallest beginning of that order with `count` logits or a weight of `target`; returns its weight.
+  auto keep = [&](uint32_t count, uint64_t target) {
+    const bool weighed = target != ~0ull || set.by_p;
+    uint32_t hi = Key::of(top), lo = Key::of(bound), before = 0, equal = 0;
+    uint64_t weight_before = 0;
+    for (bool first = true;; first = false) {
+      const int shift = sample_shift(hi - lo);
+      sample_clear(s);
+      each([&](uint32_t key, float z, uint32_t at) {
+        if (key < lo || key > hi || rank(key, at) < cut) return;
+        atomicAdd(&s.count[(hi - key) >> shift], 1u);
+        if (weighed) {
+          const uint64_t w = fixed(weight(z));
+          if (w != 0) atomicAdd(&s.weight[(hi - key) >> shift], (unsigned long long)w);
+        }
+      });
+      const SampleFound f = sample_find(s, count == ~0u ? ~0u : count - before, target == ~0ull ? ~0ull : target - weight_before);
+      if (f.bin < 0) return f.weight_all;  // (the first time alone: all are kept)
+      before += f.before;
+      weight_before += f.weight_before;
+      equal = f.count;
+      hi -= (uint32_t)f.bin << shift;
+      if (shift == 0) break;
+      lo = max(lo, hi - ((1u << shift) - 1u));
+    }
+    const uint64_t w = fixed(weight(Key::value(hi)));
+    uint64_t of_equal = count != ~0u ? count - before : (target - weight_before + w - 1) / w;
+    uint32_t last = 0xffffffffu;  // place of the last of the equal ones that is kept
+    if (of_equal < equal) {
+      uint32_t from = 0, n = (uint32_t)a.V, left = (uint32_t)of_equal;
+      for (;;) {
+        const int shift = sample_shift(n - 1);
+        sample_clear(s);
+        each([&](uint32_t key, float, uint32_t at) {
+          if (key == hi && at - from < n && rank(key, at) >= cut) atomicAdd(&s.count[(at - from) >> shift], 1u);
+        });
+        const SampleFound f = sample_find(s, left, ~0ull);
+        left -= f.before;
+        from += (uint32_t)f.bin << shift;
+        n = min(n - ((uint32_t)f.bin << shift), 1u << shift);
+        if (shift == 0) break;
+      }
+      last = from;
+    } else {
+      of_equal = equal;
+    }
+    const uint64_t from_here = rank(hi, last);
+    cut = cut > from_here ? cut : from_here;  // (all of the equal ones that an earlier cut left)
+    return weight_before + of_equal * w;
+  };
+  if (set.by_k) {
+    const uint64_t kept = keep((uint32_t)set.k, ~0ull);
+    sum = (double)kept / one;
+  }
+  if (set.by_p) {
+    const double target = ceil((double)set.p * sum * one);
+    keep(~0u, target >= 1.0 ? (uint64_t)target : 1);
+  }
+  uint64_t whole;
+  const uint32_t at = draw(0, (uint32_t)a.V, chance, each, [&](uint32_t key, float z, uint32_t place) {
+    if (z < bound || rank(key, place) < cut) return (uint64_t)0;
+    const double w = weight(z);
+    return set.by_least && w < (double)set.least ? (uint64_t)0 : fixed(w);
+  }, whole);
+  answer(at, logprob(at, (double)whole / one));
+}
+
+}  // namespace lce

@@ -1,7 +1,8 @@
 """Python binding of the operators on the vocabulary's matrix and logits (include/lce_vocab.h).
 
 In front of a model: the rows of its V x H matrix that tokens name, and their gradient, alone or added to that of an output
-layer with the same weight. Argument marshalling only, as in lce.py and ops.py: every computation runs in liblce.so's HIP
+layer with the same weight. Behind it, when it answers: the output layer's product with a weight in 4 bits, and a token from
+logits. Argument marshalling only, as in lce.py and ops.py: every computation runs in liblce.so's HIP
 kernels, on the current stream of the tensors' device, and nothing waits for the GPU.
 """
 from __future__ import annotations
@@ -16,8 +17,15 @@ from .lce import DTYPES, LCEError, load_library
 from .ops import _check_unfollowed, _pitch, _space, _upstream, _written
 
 EXPORTED = ("lce_embedding_forward", "lce_embedding_workspace_size", "lce_embedding_backward", "lce_mxfp4_quantize",
-            "lce_mxfp4_dequantize", "lce_mxfp4_matmul")
+            "lce_mxfp4_dequantize", "lce_mxfp4_matmul", "lce_sample_workspace_size", "lce_sample")
 _TOKENS = {torch.int64: 8, torch.int32: 4}
+
+class SampleSettings(ctypes.Structure):
+    """lce_sample_t."""
+
+    _fields_ = [("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float), ("top_k", ctypes.c_int32),
+                ("temperatures", ctypes.c_void_p), ("top_ps", ctypes.c_void_p), ("min_ps", ctypes.c_void_p), ("top_ks", ctypes.c_void_p)]
+
 
 _lib = None
 
@@ -34,7 +42,9 @@ def _library() -> ctypes.CDLL:
             ("lce_embedding_backward", [vp, i64, vp, ci, i64, i64, i64, ci, f32, i64, vp, i64, ci, vp, sz, vp], ci),
             ("lce_mxfp4_quantize", [vp, i64, i64, i64, ci, vp, vp, vp], ci),
             ("lce_mxfp4_dequantize", [vp, vp, i64, i64, ci, vp, i64, vp], ci),
-            ("lce_mxfp4_matmul", [vp, vp, i64, vp, vp, i64, i64, ci, vp, i64, vp], ci)]:
+            ("lce_mxfp4_matmul", [vp, vp, i64, vp, vp, i64, i64, ci, vp, i64, vp], ci),
+            ("lce_sample_workspace_size", [i64, i64], sz),
+            ("lce_sample", [vp, i64, i64, i64, ci, vp, ctypes.POINTER(SampleSettings), vp, vp, vp, sz, vp], ci)]:
         f = getattr(lib, name)
         f.argtypes, f.restype = args, res
     _lib = lib
@@ -257,3 +267,55 @@ def mxfp4_linear(hidden, weight_codes, weight_scales, out=None):
     """
     codes, scales = mxfp4_quantize(hidden)
     return mxfp4_matmul(codes, scales, weight_codes, weight_scales, hidden.dtype, out)
+
+
+# ---- a token from logits ---------------------------------------------------------------------------
+
+def _setting(v, lead, dev, dtype, what: str):
+    """(one value, a pointer to each row's)."""
+    if not isinstance(v, torch.Tensor):
+        return v, None
+    if v.shape != lead or v.dtype is not dtype or v.get_device() != dev.index or not v.is_contiguous() or v.is_neg():
+        raise ValueError(f"{what} must be a number or a contiguous tensor of {dtype} with one for each row, on the logits' device")
+    return 0, v.data_ptr()
+
+
+def sample_workspace_size(N: int, V: int) -> int:
+    """Bytes of workspace for the tokens of N rows of V logits."""
+    return int((_lib or _library()).lce_sample_workspace_size(N, V))
+
+
+def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, return_logprobs: bool = False,
+           workspace: torch.Tensor | None = None):
+    """tokens [...] (int64), or (tokens, logprobs): for each row of logits [..., V] the token that its number in uniforms [...] draws.
+
+    uniforms are fp32 in [0, 1). Logits are divided by temperature (0: the largest logit, the first of equal ones); then top_k keeps that many
+    of the largest (0: all; of equal ones the first), top_p of these as many as make up that share, and min_p of these those
+    of at least that share of the largest one's probability. The kept ones, in the order of the vocabulary, divide up [0, 1) by their probabilities,
+    and the token is the one whose part holds the row's number. Each setting is a number, or a tensor with one for each row (fp32; top_k:
+    int32). logprobs (fp32) are the logs of the tokens' probabilities among the kept ones. A row with a NaN, or with
+    nothing above -inf, gives -1. Not differentiable.
+    """
+    dev = _device_rows(logits, "logits")
+    V = logits.shape[-1] if logits.dim() else 0
+    if V < 1:
+        raise ValueError("logits must be [..., V]")
+    lead = logits.shape[:-1]
+    if uniforms.shape != lead or uniforms.dtype is not torch.float32 or uniforms.get_device() != dev.index or not uniforms.is_contiguous() or uniforms.is_neg():
+        raise ValueError("uniforms must be contiguous float32 with one for each row, on the logits' device")
+    t, ts = _setting(temperature, lead, dev, torch.float32, "temperature")
+    p, ps = _setting(top_p, lead, dev, torch.float32, "top_p")
+    m, ms = _setting(min_p, lead, dev, torch.float32, "min_p")
+    k, ks = _setting(top_k, lead, dev, torch.int32, "top_k")
+    if not (t >= 0 and p >= 0 and 0 <= m <= 1 and k >= 0):
+        raise ValueError("temperature, top_k and top_p must not be negative, min_p must be from 0 to 1")
+    N, need = logits.numel() // V, (_lib or _library()).lce_sample_workspace_size(logits.numel() // V, V)
+    if need == 0:
+        raise LCEError(2, "lce_sample_workspace_size")
+    tokens = logits.new_empty(lead, dtype=torch.int64)
+    logprobs = logits.new_empty(lead, dtype=torch.float32) if return_logprobs else None
+    ws = _space(workspace, logits, need)
+    settings = SampleSettings(t, p, m, min(k, V), ts, ps, ms, ks)
+    _call("lce_sample", dev, logits.data_ptr(), _pitch(logits, "logits"), N, V, DTYPES[logits.dtype], uniforms.data_ptr(), settings, tokens.data_ptr(),
+          None if logprobs is None else logprobs.data_ptr(), ws.data_ptr(), ws.numel())
+    return (tokens, logprobs) if return_logprobs else tokens
