@@ -117,109 +117,178 @@ __device__ __forceinline__ f32x4 mx_mfma(const u32x4& w, uint32_t ws, const u32x
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, 4, J, (int)ws, J, (int)xs);
 }
 
-// 256 values of K of a lane's row: two groups' codes and scale bytes.
-struct MxFragment {
-  u32x4 codes[2];
-  uint32_t scales;
-};
 constexpr int kMxStep = 256, kMxStepBytes = kMxStep / 2, kMxStepGroups = kMxStep / kMxGroup;
-constexpr uint32_t kMxOne = 0x7f7fu;  // two scales of 1
 
-__device__ __forceinline__ void mx_load(const uint8_t* codes, const uint8_t* scales, int step, MxFragment& f) {
-  __builtin_memcpy(&f.codes[0], codes + step * kMxStepBytes, 16);
-  __builtin_memcpy(&f.codes[1], codes + step * kMxStepBytes + 16, 16);
-  uint16_t s;
-  __builtin_memcpy(&s, scales + step * kMxStepGroups, 2);
-  f.scales = s;
+// Rows of a matrix from a tile's first one on: what lies past the last row reads as zeros.
+struct MxRows {
+  __amdgpu_buffer_rsrc_t codes, scales;
+};
+__device__ __forceinline__ MxRows mx_rows(const uint8_t* codes, const uint8_t* scales, int64_t first, int rows, uint32_t pitch, uint32_t groups) {
+  return {make_rsrc((const void*)uniform64((uint64_t)(codes + first * pitch)), __builtin_amdgcn_readfirstlane((uint32_t)rows * pitch)),
+          make_rsrc((const void*)uniform64((uint64_t)(scales + first * groups)), __builtin_amdgcn_readfirstlane((uint32_t)rows * groups))};
 }
-// The last, shorter step: groups past the row's end are zeros.
-__device__ __forceinline__ void mx_load_tail(const uint8_t* codes, const uint8_t* scales, int step, int groups, int first, MxFragment& f) {
-  f.scales = 0;
+
+// The scales of a run of steps go through LDS: a wave that loads the 8 bytes of 16 rows that a step needs waits for as many cache
+// lines as for the codes (4096 x 128256, one row of x: 64 us, 46 without scales; 64 rows 114 and 79).
+constexpr int kMxRunSteps = 32, kMxRunBytes = kMxRunSteps * kMxStepGroups, kMxRunPitch = kMxRunBytes + 16;
+
+// ROWS rows' scales of groups first .. first + bytes - 1 (of `groups` in a row).
+template <int ROWS>
+struct MxScaleRun {
+  static constexpr int kPieces = ROWS * (kMxRunBytes / 8) / 256;  // a thread's, at most
+  u32x2 piece[kPieces];
+  // Whole steps (bytes % 8 == 0): requested together, stored later. lanes, a power of two, have a row's.
+  __device__ __forceinline__ void load(const MxRows& r, uint32_t groups, int first, int bytes, int lanes) {
+    const int rows = 256 / lanes, c = (int)threadIdx.x % lanes * 8;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    f.codes[j] = (u32x4){};
-    uint32_t s = 127;
-    if (first + j < groups) {
-      __builtin_memcpy(&f.codes[j], codes + step * kMxStepBytes + 16 * j, 16);
-      s = scales[step * kMxStepGroups + j];
+    for (int k = 0; k < kPieces; ++k) {
+      if (k * rows >= ROWS) break;
+      const int row = k * rows + (int)threadIdx.x / lanes;
+      const uint32_t at = row < ROWS && c < bytes ? (uint32_t)row * groups + (uint32_t)(first + c) : kOOB;
+      piece[k] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r.scales, at, 0, 0));
     }
-    f.scales |= s << (8 * j);
   }
-}
-
-// Few rows of x (up to 16 MT): W is read once, straight into registers, and nothing else takes long. A workgroup has 32 rows
-// of W; its four waves take the steps of K in turn, the next one requested under the current one's products, and add up at
-// the end. x comes from L2: 32 rows of W for each read of it.
-template <typename T, int MT>
-__global__ __launch_bounds__(256) void mxfp4_few_kernel(const MxMatmulArgs a) {
-  constexpr int kRowsW = 32, kPitch = kRowsW + 4, kWaves = 4;
-  __shared__ float sums[kWaves][16 * MT][kPitch];
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
-  const int64_t v0 = (int64_t)blockIdx.x * kRowsW, pitch = a.K / 2, groups = a.K / kMxGroup;
-  const uint8_t *pw[2], *sw[2], *px[MT], *sx[MT];
+  __device__ __forceinline__ void store(char* lds, int lanes) {
+    const int rows = 256 / lanes, c = (int)threadIdx.x % lanes * 8;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int64_t v = min(v0 + 16 * i + row, a.V - 1);
-    pw[i] = a.w + v * pitch + 32 * quarter;
-    sw[i] = a.w_scales + v * groups + 2 * quarter;
+    for (int k = 0; k < kPieces; ++k) {
+      const int row = k * rows + (int)threadIdx.x / lanes;
+      if (k * rows < ROWS && row < ROWS) *(u32x2*)(lds + row * kMxRunPitch + c) = piece[k];
+    }
   }
+  // Any number of bytes, 4 at a time and the rest one by one, each within the row: what follows it may be no memory, or
+  // a NaN's scale.
+  static __device__ __forceinline__ void copy(const MxRows& r, uint32_t groups, int first, int bytes, char* lds) {
+    int lanes = 2;  // (a step's eight bytes at least, the last ones zeros)
+    while (lanes * 4 < bytes) lanes *= 2;
+#pragma unroll 4
+    for (int k = threadIdx.x; k < ROWS * lanes; k += 256) {
+      const int row = k / lanes, c = k % lanes * 4, left = bytes - c;
+      const uint32_t at = (uint32_t)row * groups + (uint32_t)(first + c);
+      uint32_t v = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r.scales, left >= 4 ? at : kOOB, 0, 0);
+      if (bytes % 4 != 0) {
 #pragma unroll
-  for (int j = 0; j < MT; ++j) {
-    const int64_t m = min((int64_t)16 * j + row, a.M - 1);
-    px[j] = a.x + m * pitch + 32 * quarter;
-    sx[j] = a.x_scales + m * groups + 2 * quarter;
-  }
-  f32x4 acc[2][MT] = {};
-  auto request = [&](int step, MxFragment (&w)[2], MxFragment (&x)[MT]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) mx_load(pw[i], sw[i], step, w[i]);
-#pragma unroll
-    for (int j = 0; j < MT; ++j) mx_load(px[j], sx[j], step, x[j]);
-  };
-  auto multiply = [&](const MxFragment (&w)[2], const MxFragment (&x)[MT]) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        acc[i][j] = mx_mfma<0>(w[i].codes[0], w[i].scales, x[j].codes[0], x[j].scales, acc[i][j]);
-        acc[i][j] = mx_mfma<1>(w[i].codes[1], w[i].scales, x[j].codes[1], x[j].scales, acc[i][j]);
+        for (int e = 0; e < 3; ++e)
+          v |= (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(r.scales, left > e && left < 4 ? at + e : kOOB, 0, 0) << (8 * e);
       }
-  };
-  const int steps = a.K / kMxStep;
-  if (wave < steps) {
-    // (requests past the last step read it again: behind a branch the compiler would wait for all of them)
-    MxFragment w0[2], w1[2], x0[MT], x1[MT];
-    request(wave, w0, x0);
-    for (int s = wave;;) {
-      request(min(s + kWaves, steps - 1), w1, x1);
-      multiply(w0, x0);
-      if ((s += kWaves) >= steps) break;
-      request(min(s + kWaves, steps - 1), w0, x0);
-      multiply(w1, x1);
-      if ((s += kWaves) >= steps) break;
+      *(uint32_t*)(lds + row * kMxRunPitch + c) = v;
     }
   }
-  if (a.K % kMxStep != 0 && wave == steps % kWaves) {
-    MxFragment w[2], x[MT];
-    const int left = (a.K % kMxStep) / kMxGroup;
+};
+
+// Few rows of x (up to 16 MT): W is read once, straight into registers, and nothing else takes long. A workgroup has 16 NV rows
+// of W; its four waves take the steps of K in turn, the next one requested before the current one's products, and add up at
+// the end. x comes from L2: 16 NV rows of W for each read of it. Lane quarter q takes groups q and 4 + q of a step's eight.
+template <typename T, int MT, int NV>
+__global__ __launch_bounds__(256, 2) void mxfp4_few_kernel(const MxMatmulArgs a) {
+  constexpr int kRowsW = 16 * NV, kRowsX = 16 * MT, kPitch = kRowsW + 4, kWaves = 4, kTiles = NV > MT ? NV : MT;
+  constexpr int kScales = (kRowsW + kRowsX) * kMxRunPitch, kSums = kWaves * kRowsX * kPitch * 4;
+  __shared__ __attribute__((aligned(16))) char smem[kScales > kSums ? kScales : kSums];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
+  const int64_t v0 = (int64_t)blockIdx.x * kRowsW;
+  const uint32_t pitch = (uint32_t)a.K / 2, groups = (uint32_t)a.K / kMxGroup;
+  const MxRows rw = mx_rows(a.w, a.w_scales, v0, (int)min(a.V - v0, (int64_t)kRowsW), pitch, groups);
+  const MxRows rx = mx_rows(a.x, a.x_scales, 0, (int)a.M, pitch, groups);
+  uint32_t at[kTiles];  // of both: rows 16 i + lane % 16
 #pragma unroll
-    for (int i = 0; i < 2; ++i) mx_load_tail(pw[i], sw[i], steps, left, 2 * quarter, w[i]);
+  for (int i = 0; i < kTiles; ++i) at[i] = (uint32_t)(16 * i + row) * pitch + 16 * quarter;
+  f32x4 acc[NV][MT] = {};
+  struct Step {
+    u32x4 w[NV][2], x[MT][2];
+  };
+  auto request = [&](int step, Step& b) {
+    const uint32_t k = (uint32_t)step * kMxStepBytes;
 #pragma unroll
-    for (int j = 0; j < MT; ++j) mx_load_tail(px[j], sx[j], steps, left, 2 * quarter, x[j]);
-    multiply(w, x);
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) b.w[i][h] = load16(rw.codes, at[i] + 64 * h, k);
+#pragma unroll
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) b.x[j][h] = load16(rx.codes, at[j] + 64 * h, k);
+    __builtin_amdgcn_sched_barrier(0);  // (the compiler would move the requests down to their use)
+  };
+  const char* scales_w = smem + row * kMxRunPitch;
+  const char* scales_x = scales_w + kRowsW * kMxRunPitch;
+  auto multiply = [&](const Step& b, int step) {  // step: of the run
+    u32x2 sw[NV], sx[MT];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) sw[i] = *(const u32x2*)(scales_w + 16 * i * kMxRunPitch + step * kMxStepGroups) >> (uint32_t)(8 * quarter);
+#pragma unroll
+    for (int j = 0; j < MT; ++j) sx[j] = *(const u32x2*)(scales_x + 16 * j * kMxRunPitch + step * kMxStepGroups) >> (uint32_t)(8 * quarter);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j) acc[i][j] = mx_mfma<0>(b.w[i][h], sw[i][h], b.x[j][h], sx[j][h], acc[i][j]);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const int steps = a.K / kMxStep;  // whole ones
+  for (int s0 = 0; s0 * kMxStep < a.K; s0 += kMxRunSteps) {
+    const int end = min(steps, s0 + kMxRunSteps), bytes = min(kMxRunBytes, (int)groups - s0 * kMxStepGroups);
+    int lanes = 1;
+    while (lanes * 8 < bytes) lanes *= 2;
+    MxScaleRun<kRowsW> run_w;
+    MxScaleRun<kRowsX> run_x;
+    const bool pieces = bytes % 8 == 0;
+    if (pieces) {
+      run_w.load(rw, groups, s0 * kMxStepGroups, bytes, lanes);
+      run_x.load(rx, groups, s0 * kMxStepGroups, bytes, lanes);
+    }
+    int s = s0 + wave;
+    Step b0, b1;
+    if (s < end) request(s, b0);
+    if (s0 > 0) __syncthreads();
+    if (pieces) {
+      run_w.store(smem, lanes);
+      run_x.store(smem + kRowsW * kMxRunPitch, lanes);
+    } else {
+      MxScaleRun<kRowsW>::copy(rw, groups, s0 * kMxStepGroups, bytes, smem);
+      MxScaleRun<kRowsX>::copy(rx, groups, s0 * kMxStepGroups, bytes, smem + kRowsW * kMxRunPitch);
+    }
+    __syncthreads();
+    if (s < end) {
+      // (requests past the last step read it again: behind a branch the compiler would wait for all of them)
+      for (;;) {
+        request(min(s + kWaves, end - 1), b1);
+        multiply(b0, s - s0);
+        if ((s += kWaves) >= end) break;
+        request(min(s + kWaves, end - 1), b0);
+        multiply(b1, s - s0);
+        if ((s += kWaves) >= end) break;
+      }
+    }
+    // The last, shorter step: groups past the row's end are zeros.
+    if (end == steps && steps - s0 < kMxRunSteps && a.K % kMxStep != 0 && wave == steps % kWaves) {
+      const int left = a.K % kMxStep / kMxGroup;
+      const uint32_t k = (uint32_t)steps * kMxStepBytes;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool in = quarter + 4 * h < left;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) b0.w[i][h] = load16(rw.codes, in ? at[i] + 64 * h + k : kOOB);
+#pragma unroll
+        for (int j = 0; j < MT; ++j) b0.x[j][h] = load16(rx.codes, in ? at[j] + 64 * h + k : kOOB);
+      }
+      multiply(b0, steps - s0);
+    }
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < MT; ++j) *(f32x4*)&sums[wave][16 * j + row][16 * i + 4 * quarter] = acc[i][j];
   __syncthreads();
+  float* sums = (float*)smem;  // [wave][row of x][row of W]
 #pragma unroll
-  for (int k = 0; k < MT; k += 2) {
-    const int m = 16 * k + (int)threadIdx.x / 8, c = threadIdx.x % 8 * 4;
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int j = 0; j < MT; ++j) *(f32x4*)&sums[(wave * kRowsX + 16 * j + row) * kPitch + 16 * i + 4 * quarter] = acc[i][j];
+  __syncthreads();
+  constexpr int kRowLanes = kRowsW / 4, kRows = 256 / kRowLanes;  // threads that share a row of the result
+#pragma unroll
+  for (int k = 0; k < 16 * MT; k += kRows) {
+    const int m = k + (int)threadIdx.x / kRowLanes, c = threadIdx.x % kRowLanes * 4;
     if (m >= 16 * MT || m >= a.M) break;
-    f32x4 y = *(f32x4*)&sums[0][m][c];
+    f32x4 y = *(f32x4*)&sums[m * kPitch + c];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) y += *(f32x4*)&sums[w][m][c];
+    for (int w = 1; w < kWaves; ++w) y += *(f32x4*)&sums[(w * kRowsX + m) * kPitch + c];
     T* p = (T*)a.out + m * a.out_ld + v0 + c;
     T q[4] = {from_f32<T>(y[0]), from_f32<T>(y[1]), from_f32<T>(y[2]), from_f32<T>(y[3])};
     if (v0 + c + 4 <= a.V) {

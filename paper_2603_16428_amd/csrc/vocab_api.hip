@@ -146,12 +146,16 @@ lce_status_t run_mxfp4_many(MxMatmulArgs a, hipStream_t s) {
 
 template <typename T>
 lce_status_t run_mxfp4_matmul(const MxMatmulArgs& a, hipStream_t s) {
-  if (a.M > 64) return a.M <= 128 ? run_mxfp4_many<T, 128>(a, s) : run_mxfp4_many<T, 256>(a, s);
-  const dim3 grid((unsigned)cdiv(a.V, 32));
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
-  if (a.M <= 16) go(mxfp4_few_kernel<T, 1>);
-  else if (a.M <= 32) go(mxfp4_few_kernel<T, 2>);
-  else go(mxfp4_few_kernel<T, 4>);
+  // Few rows read W straight into registers. From 49 on the tile of 128 is the faster (4096 x 128256: 48 rows 76 us, 64 rows
+  // 89 us so and 85 in the tile, which takes 90 for 128).
+  if (a.M > 48) return a.M <= 128 ? run_mxfp4_many<T, 128>(a, s) : run_mxfp4_many<T, 256>(a, s);
+  // 64 rows of W a workgroup read x half as often as 32 (4096 x 128256: 32 rows 68 us against 79, one 51 against 48), if they
+  // still leave each CU a workgroup.
+  const bool wide = a.M > 4 && a.V >= 64 * 256;
+  auto go = [&](auto kernel, int rows) { hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv(a.V, rows)), dim3(256), 0, s, a); };
+  if (a.M <= 16) wide ? go(mxfp4_few_kernel<T, 1, 4>, 64) : go(mxfp4_few_kernel<T, 1, 2>, 32);
+  else if (a.M <= 32) wide ? go(mxfp4_few_kernel<T, 2, 4>, 64) : go(mxfp4_few_kernel<T, 2, 2>, 32);
+  else wide ? go(mxfp4_few_kernel<T, 3, 4>, 64) : go(mxfp4_few_kernel<T, 3, 2>, 32);
   return launched();
 }
 
