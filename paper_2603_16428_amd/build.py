@@ -3,8 +3,8 @@
     python -m paper_2603_16428_amd.build
 
 compiles csrc/lce_api.hip (which includes the step's kernels), csrc/ops_api.hip (the operators around
-the step), csrc/vocab_api.hip (those on the vocabulary's matrix and logits) and csrc/host_adam.cpp (the host
-optimizer step) into liblce.so next to this file.
+the step), csrc/embedding_api.hip, csrc/mxfp4_api.hip and csrc/sample_api.hip (those on the vocabulary's matrix and
+logits) and csrc/host_adam.cpp (the host optimizer step) into liblce.so next to this file.
 """
 from __future__ import annotations
 
@@ -18,7 +18,7 @@ ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "liblce.so")
 KERNEL_SOURCES = [os.path.join(HERE, "csrc", "lce_api.hip")]
 OPS_SOURCES = [os.path.join(HERE, "csrc", "ops_api.hip")]
-VOCAB_SOURCES = [os.path.join(HERE, "csrc", "vocab_api.hip")]
+VOCAB_SOURCES = [os.path.join(HERE, "csrc", name) for name in ("embedding_api.hip", "mxfp4_api.hip", "sample_api.hip")]
 HOST_SOURCES = [os.path.join(HERE, "csrc", "host_adam.cpp")]
 SOURCES = KERNEL_SOURCES + OPS_SOURCES + VOCAB_SOURCES + HOST_SOURCES
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

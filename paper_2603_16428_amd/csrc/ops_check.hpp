@@ -7,6 +7,7 @@
 #include <utility>
 
 #include "lce.h"
+#include "lce_gemm.hpp"
 
 namespace lce {
 namespace {
@@ -14,6 +15,13 @@ namespace {
 int64_t cdiv(int64_t x, int64_t m) { return (x + m - 1) / m; }
 bool dtype_ok(int dtype) { return dtype == LCE_DTYPE_FP32 || dtype == LCE_DTYPE_BF16 || dtype == LCE_DTYPE_FP16; }
 int64_t size_of(int dtype) { return dtype == LCE_DTYPE_FP32 ? 4 : 2; }
+// Calls f with a value of the element type.
+template <typename F>
+lce_status_t by_type(int dtype, F f) {
+  if (dtype == LCE_DTYPE_BF16) return f(bf16{});
+  if (dtype == LCE_DTYPE_FP16) return f(f16{});
+  return f(float{});
+}
 lce_status_t launched() { return hipGetLastError() == hipSuccess ? LCE_OK : LCE_ERR_HIP; }
 
 // ---- row tensors ----
@@ -37,6 +45,8 @@ bool overlap(const Rows& a, const Rows& b) {
 }
 bool same(const Rows& a, const Rows& b) { return a.p == b.p && (a.pitch == b.pitch || a.N == 1) && a.row == b.row; }
 
+// Workgroups at most of kernels that walk on over rows.
+constexpr int64_t kRowBlocks = int64_t(1) << 20;
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1, kMaxPitch = int64_t(1) << 30;
 
 // Pitch and alignment of rows (`size`: bytes of an element).
