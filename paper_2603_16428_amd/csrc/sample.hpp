@@ -8,7 +8,9 @@
 //
 // Two launches: parts of a row in parallel (the maximum of each group of 64 logits, sums of weights where the whole row's
 // is needed), then a workgroup per row. Its settings and the groups' maxima give a bound that no kept logit is below: only
-// groups above it are read again, and, where few logits pass, they are listed in LDS.
+// groups above it are read again, and, where few logits pass, they are listed in LDS. Where top-p (or a top-k beyond the number of
+// groups) may keep very many, each part also leaves a table of counts and weights by cells of T / 4: the cell where the target is
+// reached is then known without reading the row, and only that cell's logits are listed.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -17,6 +19,7 @@
 
 namespace lce {
 
+constexpr int kSampleCells = 128;  // of a quarter of T: the last one's weights are 2^-46
 constexpr int kSampleParts = 64, kPartGroups = 64, kMostGroups = kSampleParts * kPartGroups;
 
 struct SampleArgs {
@@ -31,6 +34,8 @@ struct SampleArgs {
   float* logprobs;
   float *group_max, *part_max;  // [N][groups], [N][parts]
   double* part_sum;             // [N][parts], relative to the part's maximum
+  uint64_t* cell_weight;        // [N][parts][cells], relative to the part's maximum (rows for which cells() is true)
+  uint32_t* cell_count;
   int V, groups, parts, bits;   // bits: a weight of 1 is 2^bits
 };
 
@@ -38,10 +43,11 @@ struct SampleRow {
   double rate;  // 256 log2(e) / T
   float T, p, least;
   int k;  // 0: all
-  bool greedy, by_k, by_p, by_least;
+  // cells: so many may be kept that their weights and counts are tabled.
+  bool greedy, by_k, by_p, by_least, cells;
   __device__ __forceinline__ bool whole() const { return !by_k && !by_p && !by_least; }
   // Whether the sum of the whole row's weights is needed.
-  __device__ __forceinline__ bool sums() const { return !greedy && !by_k && (by_p || whole()); }
+  __device__ __forceinline__ bool sums() const { return !greedy && (cells || (!by_k && (by_p || whole()))); }
 };
 __device__ __forceinline__ SampleRow sample_row(const SampleArgs& a, int64_t i) {
   SampleRow r;
@@ -53,6 +59,7 @@ __device__ __forceinline__ SampleRow sample_row(const SampleArgs& a, int64_t i) 
   r.by_k = r.k > 0 && r.k < a.V;
   r.by_p = r.p < 1.f;
   r.by_least = r.least > 0.f;
+  r.cells = !r.greedy && !r.by_least && (r.by_k ? r.k > a.groups : r.by_p);
   r.rate = 256.0 * 1.4426950408889634074 / (double)r.T;
   return r;
 }
@@ -75,6 +82,13 @@ __device__ __forceinline__ double sample_weight(float z, float top, double rate,
   return z == top ? 1.0 : w;
 }
 
+// How many cells below the larger `top` z is, up to kSampleCells. Cells lie at multiples of T / 4, the same for every part.
+__device__ __forceinline__ int sample_cell(float z, float top, double rate) {
+  const double c = rate * (4.0 / (256.0 * 1.4426950408889634074));  // 4 / T
+  const double d = floor((double)top * c) - floor((double)z * c);
+  return z == top ? 0 : d < (double)kSampleCells ? (int)d : kSampleCells;
+}
+
 // The larger of two, and NaN if one is.
 __device__ __forceinline__ float max_or_nan(float a, float b) { return (a >= b || a != a) ? a : b; }
 
@@ -84,6 +98,8 @@ __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleArgs a) {
   constexpr int kGroup = 64 * REP, kRounds = kPartGroups / 32;
   __shared__ double table[256], sums[4];
   __shared__ float tops[4];
+  __shared__ unsigned long long cell_weight[kSampleCells];
+  __shared__ uint32_t cell_count[kSampleCells];
   const int64_t i = blockIdx.x / a.parts;
   const int part = blockIdx.x % a.parts;
   const T* row = (const T*)a.logits + i * a.ld;
@@ -99,6 +115,7 @@ __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleArgs a) {
       load_raw<END>(row + at, a.V - at, raw[g][r]);
     }
   if (summed) sample_table(table);
+  if (threadIdx.x < kSampleCells) cell_weight[threadIdx.x] = cell_count[threadIdx.x] = 0;
   float top = -INFINITY;
   auto count_of = [&](int g, int r) {  // logits of this piece
     return a.V - ((part * kPartGroups + g * 32 + (int)threadIdx.x / 8) * kGroup + r * 64 + ((int)threadIdx.x % 8) * kNormVec);
@@ -133,7 +150,18 @@ __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleArgs a) {
       for (int r = 0; r < REP; ++r)
 #pragma unroll
         for (int e = 0; e < kNormVec; ++e)
-          if (e < count_of(g, r)) sum += sample_weight(raw[g][r].at(e), top, set.rate, table);
+          if (e < count_of(g, r)) {
+            const float z = raw[g][r].at(e);
+            const double w = sample_weight(z, top, set.rate, table);
+            sum += w;
+            if (set.cells) {
+              const int cell = sample_cell(z, top, set.rate);
+              if (cell < kSampleCells) {
+                atomicAdd(&cell_weight[cell], (unsigned long long)(uint64_t)fma(w, 0x1p44, 0.5));
+                atomicAdd(&cell_count[cell], 1u);
+              }
+            }
+          }
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
@@ -142,6 +170,10 @@ __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleArgs a) {
   if (threadIdx.x == 0) {
     a.part_max[i * a.parts + part] = top;
     a.part_sum[i * a.parts + part] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  }
+  if (set.cells && threadIdx.x < kSampleCells) {
+    a.cell_weight[(i * a.parts + part) * kSampleCells + threadIdx.x] = cell_weight[threadIdx.x];
+    a.cell_count[(i * a.parts + part) * kSampleCells + threadIdx.x] = cell_count[threadIdx.x];
   }
 }
 
@@ -161,7 +193,7 @@ struct SampleKey {
   }
 };
 
-constexpr int kSampleThreads = 1024, kSampleBins = 2 * kSampleThreads, kSampleList = 4096;
+constexpr int kSampleThreads = 1024, kSampleBins = 2 * kSampleThreads, kSampleList = 8192, kSampleFew = 256;
 
 struct SampleFound {
   int bin;  // -1: the target is not reached
@@ -178,6 +210,7 @@ struct SampleLds {
   uint32_t wave_count[16];
   float wave_max[16];
   uint32_t actives, listed, lowest;
+  unsigned long long kept;
   SampleFound found;
 };
 
@@ -360,6 +393,22 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
   };
   const double chance = u > 0.f ? (double)u : 0.0;
 
+  // Falling logits, equal ones by their places: place and key in one number. Kept are those from `cut` on.
+  auto rank = [](uint32_t key, uint32_t at) { return (uint64_t)key << 32 | (0xffffffffu - at); };
+  uint64_t cut = 0;
+  int cell = -1;  // the listed logits' cell, the last of which some are kept (-1: no cell)
+  // The token of the part in which the running weight of the parts passes `chance`, relative to the part's own maximum.
+  auto draw_in = [&](const SampleFound& f) {
+    const float of = a.part_max[i * a.parts + f.bin];
+    const double inside = (fmin(chance, 1.0) * (double)f.weight_all - (double)f.weight_before) / (double)f.weight;
+    const uint32_t lo = (uint32_t)f.bin * kPartGroups * kGroup, n = min((uint32_t)(kPartGroups * kGroup), (uint32_t)a.V - lo);
+    uint64_t whole;
+    const uint32_t at = draw(lo, n, fmin(fmax(inside, 0.0), 1.0), [&](auto add) { range(lo, n, add); }, [&](uint32_t key, float z, uint32_t place) {
+      return rank(key, place) < cut || (cell >= 0 && sample_cell(z, top, set.rate) > cell) ? (uint64_t)0 : fixed(sample_weight(z, of, set.rate, s.table));
+    }, whole);
+    answer(at, logprob(at, (double)f.weight_all / one));
+  };
+
   // The whole row's weight from its parts'.
   double sum = 0.0;
   if (set.sums()) {
@@ -370,59 +419,14 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
     }
     const SampleFound f = sample_find(s, ~0u, 0, chance);
     sum = (double)f.weight_all / one;
-    if (set.whole()) {
-      // Inside the part, relative to its own maximum.
-      const float of = a.part_max[i * a.parts + f.bin];
-      const double inside = (fmin(chance, 1.0) * (double)f.weight_all - (double)f.weight_before) / (double)f.weight;
-      const uint32_t lo = (uint32_t)f.bin * kPartGroups * kGroup, n = min((uint32_t)(kPartGroups * kGroup), (uint32_t)a.V - lo);
-      uint64_t whole;
-      const uint32_t at = draw(lo, n, fmin(fmax(inside, 0.0), 1.0), [&](auto add) { range(lo, n, add); },
-                               [&](uint32_t, float z, uint32_t) { return fixed(sample_weight(z, of, set.rate, s.table)); }, whole);
-      return answer(at, logprob(at, sum));
-    }
+    if (set.whole()) return draw_in(f);
   }
 
-  // No kept logit is below `bound`.
+  auto weight = [&](float z) { return sample_weight(z, top, set.rate, s.table); };
+  // No kept logit that is looked for is below `bound`.
   float bound = -INFINITY;
-  if (set.by_k && set.k <= a.groups && top < INFINITY) {
-    // The k-th largest of the groups' maxima: k logits at least are as large.
-    float least = INFINITY;
-#pragma unroll
-    for (int k = 0; k < kEach; ++k)
-      if (maxima[k] > -INFINITY) least = fminf(least, maxima[k]);
-    least = -sample_block_max(-least, s);
-    const float inv = top > least ? (float)(kSampleBins - 1) / (top - least) : 0.f;
-    if (inv < INFINITY && top - least < INFINITY) {
-      auto bin = [&](float m) { return min((int)((top - m) * inv), kSampleBins - 1); };
-      sample_clear(s);
-#pragma unroll
-      for (int k = 0; k < kEach; ++k)
-        if (maxima[k] > -INFINITY) atomicAdd(&s.count[bin(maxima[k])], 1u);
-      const SampleFound f = sample_find(s, (uint32_t)set.k, ~0ull);
-      if (f.bin >= 0) {
-        float lowest = INFINITY;
-#pragma unroll
-        for (int k = 0; k < kEach; ++k)
-          if (maxima[k] > -INFINITY && bin(maxima[k]) <= f.bin) lowest = fminf(lowest, maxima[k]);
-        bound = -sample_block_max(-lowest, s);
-      }
-    }
-  }
-  // Those of a weight below w: (with room for the rounding of this bound)
-  auto bound_of = [&](double w) {
-    const double b = (double)top + (double)set.T * log(w);
-    return (float)(b - 1e-6 * fabs(b) - 1e-6 * (double)set.T);
-  };
-  if (set.by_least && !(set.by_k && set.by_p)) bound = fmaxf(bound, bound_of((double)set.least));
-  // Those below (1 - p) Z / V together weigh less than (1 - p) Z.
-  if (set.by_p && set.p <= 0.f) bound = top;
-  else if (set.by_p && !set.by_k) bound = fmaxf(bound, bound_of((1.0 - (double)set.p) * sum / (double)a.V));
-
-#pragma unroll
-  for (int k = 0; k < kEach; ++k)
-    if (maxima[k] >= bound && tid + k * kSampleThreads < a.groups) s.active[atomicAdd(&s.actives, 1u)] = (uint16_t)(tid + k * kSampleThreads);
-  __syncthreads();
-  const int actives = (int)s.actives;
+  int actives = 0;
+  uint32_t listed = 0;
   // The logits of the active groups that are not below the bound: eight lanes a group, four groups requested at once.
   auto stream = [&](auto f) {
     constexpr int kAhead = 4, kAtOnce = kSampleThreads / 8;
@@ -450,15 +454,27 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
       }
     }
   };
-  stream([&](uint32_t key, float, uint32_t at) {
-    const uint32_t k = atomicAdd(&s.listed, 1u);
-    if (k < (uint32_t)kSampleList) {
-      s.list_key[k] = key;
-      s.list_at[k] = at;
-    }
-  });
-  __syncthreads();
-  const uint32_t listed = s.listed;
+  // Lists the logits that are not below the bound (those of the cell alone).
+  auto list = [&]() {
+    __syncthreads();
+    if (tid == 0) s.actives = s.listed = 0;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (maxima[k] >= bound && tid + k * kSampleThreads < a.groups) s.active[atomicAdd(&s.actives, 1u)] = (uint16_t)(tid + k * kSampleThreads);
+    __syncthreads();
+    actives = (int)s.actives;
+    stream([&](uint32_t key, float z, uint32_t at) {
+      if (cell >= 0 && sample_cell(z, top, set.rate) != cell) return;
+      const uint32_t k = atomicAdd(&s.listed, 1u);
+      if (k < (uint32_t)kSampleList) {
+        s.list_key[k] = key;
+        s.list_at[k] = at;
+      }
+    });
+    __syncthreads();
+    listed = s.listed;
+  };
   auto each = [&](auto f) {
     if (listed <= (uint32_t)kSampleList) {
       for (uint32_t k = tid; k < listed; k += kSampleThreads) f(s.list_key[k], Key::value(s.list_key[k]), s.list_at[k]);
@@ -466,16 +482,88 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
       stream(f);
     }
   };
-  auto weight = [&](float z) { return sample_weight(z, top, set.rate, s.table); };
+  // (with room for the rounding of these bounds)
+  auto below = [&](double b) { return (float)(b - 1e-6 * fabs(b) - 1e-6 * (double)set.T); };
+  auto bound_of = [&](double w) { return below((double)top + (double)set.T * log(w)); };  // logits below it weigh less than w
+  auto find_bound = [&]() {
+    bound = -INFINITY;
+    if (set.by_k && set.k <= a.groups && top < INFINITY) {
+      // The k-th largest of the groups' maxima: k logits at least are as large.
+      float least = INFINITY;
+#pragma unroll
+      for (int k = 0; k < kEach; ++k)
+        if (maxima[k] > -INFINITY) least = fminf(least, maxima[k]);
+      least = -sample_block_max(-least, s);
+      const float inv = top > least ? (float)(kSampleBins - 1) / (top - least) : 0.f;
+      if (inv < INFINITY && top - least < INFINITY) {
+        auto bin = [&](float m) { return min((int)((top - m) * inv), kSampleBins - 1); };
+        sample_clear(s);
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+          if (maxima[k] > -INFINITY) atomicAdd(&s.count[bin(maxima[k])], 1u);
+        const SampleFound f = sample_find(s, (uint32_t)set.k, ~0ull);
+        if (f.bin >= 0) {
+          float lowest = INFINITY;
+#pragma unroll
+          for (int k = 0; k < kEach; ++k)
+            if (maxima[k] > -INFINITY && bin(maxima[k]) <= f.bin) lowest = fminf(lowest, maxima[k]);
+          bound = -sample_block_max(-lowest, s);
+        }
+      }
+    }
+    if (set.by_least && !(set.by_k && set.by_p)) bound = fmaxf(bound, bound_of((double)set.least));
+    // Those below (1 - p) Z / V together weigh less than (1 - p) Z.
+    if (set.by_p && set.p <= 0.f) bound = top;
+    else if (set.by_p && !set.by_k) bound = fmaxf(bound, bound_of((1.0 - (double)set.p) * sum / (double)a.V));
+  };
+  auto share_of = [&](double whole) {  // top-p's weight
+    const double target = ceil((double)set.p * whole);
+    return target >= 1.0 ? (uint64_t)target : (uint64_t)1;
+  };
 
-  // Falling logits, equal ones by their places: place and key in one number. Kept are those from `cut` on.
-  auto rank = [](uint32_t key, uint32_t at) { return (uint64_t)key << 32 | (0xffffffffu - at); };
-  uint64_t cut = 0;
-  // Makes the cut at the smallest beginning of that order with `count` logits or a weight of `target`; returns its weight.
-  auto keep = [&](uint32_t count, uint64_t target) {
+  // Few logits (a thread each): every one looks at all others.
+  auto few = [&]() {
+    const bool mine = tid < (int)listed;
+    const uint32_t key = mine ? s.list_key[tid] : 0u, at = mine ? s.list_at[tid] : ~0u;
+    const double share = mine ? weight(Key::value(key)) : 0.0;
+    const uint64_t w = fixed(share), order = rank(key, at);
+    if (mine) s.weight[tid] = w;
+    if (tid == 0) s.kept = 0;
+    __syncthreads();
+    uint64_t before = 0;
+    uint32_t ahead = 0;
+    if (mine)
+      for (uint32_t k = 0; k < listed; ++k) {
+        const bool first = rank(s.list_key[k], s.list_at[k]) > order;
+        before += first ? s.weight[k] : 0;
+        ahead += first;
+      }
+    bool kept = mine && (!set.by_k || ahead < (uint32_t)set.k);
+    if (kept && w != 0) atomicAdd(&s.kept, (unsigned long long)w);
+    __syncthreads();
+    if (set.by_p) kept = kept && before < share_of(set.by_k ? (double)s.kept : sum * one);
+    if (set.by_least) kept = kept && share >= (double)set.least;
+    if (mine) s.weight[tid] = kept ? w : 0;
+    __syncthreads();
+    if (!kept) return;
+    uint64_t up_to = 0, all = 0;
+    for (uint32_t k = 0; k < listed; ++k) {
+      up_to += s.list_at[k] <= at ? s.weight[k] : 0;
+      all += s.weight[k];
+    }
+    uint64_t target = (uint64_t)(fmin(chance, 1.0) * (double)all) + 1;
+    target = target > all ? all : target;
+    if (up_to >= target && up_to - w < target) {
+      a.tokens[i] = at;
+      if (a.logprobs != nullptr) a.logprobs[i] = logprob(at, (double)all / one);
+    }
+  };
+
+  // Makes the cut at the smallest beginning of that order with `count` logits or a weight of `target`, of which `before` and
+  // `weight_before` are not among those listed; returns its weight.
+  auto keep = [&](uint32_t count, uint64_t target, uint32_t before, uint64_t weight_before) {
     const bool weighed = target != ~0ull || set.by_p;
-    uint32_t hi = Key::of(top), lo = Key::of(bound), before = 0, equal = 0;
-    uint64_t weight_before = 0;
+    uint32_t hi = Key::of(top), lo = Key::of(bound), equal = 0;
     for (bool first = true;; first = false) {
       const int shift = sample_shift(hi - lo);
       sample_clear(s);
@@ -488,7 +576,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
         }
       });
       const SampleFound f = sample_find(s, count == ~0u ? ~0u : count - before, target == ~0ull ? ~0ull : target - weight_before);
-      if (f.bin < 0) return f.weight_all;  // (the first time alone: all are kept)
+      if (f.bin < 0) return weight_before + f.weight_all;  // (the first time alone: all are kept)
       before += f.before;
       weight_before += f.weight_before;
       equal = f.count;
@@ -521,13 +609,69 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
     cut = cut > from_here ? cut : from_here;  // (all of the equal ones that an earlier cut left)
     return weight_before + of_equal * w;
   };
-  if (set.by_k) {
-    const uint64_t kept = keep((uint32_t)set.k, ~0ull);
-    sum = (double)kept / one;
+  // The parts' tables: f(part, the row's cell, count, weight).
+  auto tables = [&](auto f) {
+    for (int k = tid; k < a.parts * kSampleCells; k += kSampleThreads) {
+      const int part = k / kSampleCells;
+      const int64_t at = (i * a.parts + part) * kSampleCells + k % kSampleCells;
+      const uint32_t n = a.cell_count[at];
+      const uint64_t w = a.cell_weight[at];
+      const float of = a.part_max[i * a.parts + part];
+      const int c = sample_cell(of, top, set.rate) + k % kSampleCells;
+      if (n != 0 && c < kSampleCells) f(part, c, n, (uint64_t)((double)w * 0x1p-44 * weight(of) * one + 0.5));
+    }
+  };
+  bool by_cells = set.cells, ready = false;
+  const double of_row = sum;
+#pragma nounroll
+  for (int what = 0; what < 3; ++what) {  // top-k, then top-p
+    if (!by_cells && !ready) {
+      find_bound();
+      list();
+      ready = true;
+      if (listed <= (uint32_t)kSampleFew) return few();
+    }
+    if (what == 0 ? !set.by_k : what == 1 ? !set.by_p : true) continue;
+    const uint32_t count = what == 0 ? (uint32_t)set.k : ~0u;
+    const uint64_t target = what == 0 ? ~0ull : share_of(sum * one);
+    uint32_t before = 0;
+    uint64_t weight_before = 0;
+    if (by_cells) {
+      sample_clear(s);
+      tables([&](int, int c, uint32_t n, uint64_t w) {
+        atomicAdd(&s.count[c], n);
+        atomicAdd(&s.weight[c], (unsigned long long)w);
+      });
+      const SampleFound f = sample_find(s, count, target);
+      if (f.bin < 0) continue;  // all weights that count are kept
+      before = f.before;
+      weight_before = f.weight_before;
+      cell = f.bin;
+      const double c = set.rate * (4.0 / (256.0 * 1.4426950408889634074));
+      bound = top < INFINITY ? below((floor((double)top * c) - cell) / c) : top;
+      list();
+      if (listed > (uint32_t)kSampleList) {  // too many logits in one cell: the long way
+        by_cells = false;
+        cell = -1;
+        cut = 0;
+        sum = of_row;
+        what = -1;
+        continue;
+      }
+    }
+    const uint64_t kept = keep(count, target, before, weight_before);
+    if (what == 0) sum = (double)kept / one;
   }
-  if (set.by_p) {
-    const double target = ceil((double)set.p * sum * one);
-    keep(~0u, target >= 1.0 ? (uint64_t)target : 1);
+  if (by_cells) {
+    sample_clear(s);
+    tables([&](int part, int c, uint32_t, uint64_t w) {
+      if (cell < 0 || c < cell) atomicAdd(&s.weight[part], (unsigned long long)w);
+    });
+    if (cell >= 0)
+      each([&](uint32_t key, float z, uint32_t at) {
+        if (rank(key, at) >= cut) atomicAdd(&s.weight[at / (kPartGroups * kGroup)], (unsigned long long)fixed(weight(z)));
+      });
+    return draw_in(sample_find(s, ~0u, 0, chance));
   }
   uint64_t whole;
   const uint32_t at = draw(0, (uint32_t)a.V, chance, each, [&](uint32_t key, float z, uint32_t place) {

@@ -35,7 +35,7 @@ size_t lce_sample_workspace_size(int64_t N, int64_t V) {
   using namespace lce;
   if (check_sample(N, V) != LCE_OK) return 0;
   const int64_t groups = cdiv(V, 64 * sample_rep(V)), parts = cdiv(groups, kPartGroups), n = std::max<int64_t>(N, 1);
-  return (size_t)cdiv(n * (parts * 12 + groups * 4), 256) * 256;
+  return (size_t)cdiv(n * (parts * (12 + 12 * kSampleCells) + groups * 4), 256) * 256;
 }
 
 lce_status_t lce_sample(const void* logits, int64_t logits_ld, int64_t N, int64_t V, int dtype, const float* uniforms,
@@ -63,11 +63,13 @@ lce_status_t lce_sample(const void* logits, int64_t logits_ld, int64_t N, int64_
   if (st != LCE_OK) return st;
   const int rep = sample_rep(V), groups = (int)cdiv(V, 64 * rep), parts = (int)cdiv(groups, kPartGroups);
   double* sums = (double*)workspace;
-  float* part_max = (float*)(sums + N * parts);
+  uint64_t* cell_weight = (uint64_t*)(sums + N * parts);
+  uint32_t* cell_count = (uint32_t*)(cell_weight + N * parts * kSampleCells);
+  float* part_max = (float*)(cell_count + N * parts * kSampleCells);
   // All weights together stay below 2^63, one below 2^51.
   const int bits = std::min(50, 62 - (V > 1 ? 32 - __builtin_clz((unsigned)(V - 1)) : 0));
   const SampleArgs a{logits, logits_ld, uniforms, c.temperature, c.top_p, c.min_p, c.top_k, c.temperatures, c.top_ps, c.min_ps, c.top_ks, tokens, logprobs,
-                     part_max + N * parts, part_max, sums, (int)V, groups, parts, bits};
+                     part_max + N * parts, part_max, sums, cell_weight, cell_count, (int)V, groups, parts, bits};
   hipStream_t s = (hipStream_t)stream;
   return by_type(dtype, [&](auto zero) {
     using T = decltype(zero);
