@@ -208,11 +208,57 @@ struct SampleLds {
   uint16_t active[kMostGroups];
   uint64_t wave_weight[16];
   uint32_t wave_count[16];
-  float wave_max[16];
+  float wave_max[16], wave_least[16];
   uint32_t actives, listed, lowest;
   unsigned long long kept;
   SampleFound found;
 };
+
+// Sums over a wave's lanes up to and with each one, by lane moves within the vector unit (a shuffle through LDS is ten times as long, and
+// what one row waits for is the chain of these).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <typename F>
+__device__ __forceinline__ void for_row_steps(F f) {
+  using std::integral_constant;
+  f(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});  // row_shr:1, 2, 4, 8: within 16 lanes
+  f(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  f(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  f(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+}
+template <typename F>
+__device__ __forceinline__ void for_scan_steps(F f) {
+  using std::integral_constant;
+  for_row_steps(f);
+  f(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});  // row_bcast:15, 31: the rows before
+  f(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t moved(uint64_t v) {
+  return (uint64_t)moved<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | moved<CTRL, ROWS>((uint32_t)v);
+}
+template <typename V>
+__device__ __forceinline__ V wave_scan(V v) {
+  for_scan_steps([&](auto c, auto r) { v += moved<decltype(c)::value, decltype(r)::value>(v); });
+  return v;
+}
+template <typename V>
+__device__ __forceinline__ V row_scan(V v) {
+  for_row_steps([&](auto c, auto r) { v += moved<decltype(c)::value, decltype(r)::value>(v); });
+  return v;
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ uint64_t lane_of(uint64_t v, int lane) { return (uint64_t)lane_of((uint32_t)(v >> 32), lane) << 32 | lane_of((uint32_t)v, lane); }
+// The wave's largest (a NaN if there is one), for all lanes.
+__device__ __forceinline__ float wave_max(float v) {
+  for_scan_steps([&](auto c, auto r) {
+    const int b = __builtin_bit_cast(int, v);  // (lanes without a partner take their own)
+    v = max_or_nan(__builtin_bit_cast(float, __builtin_amdgcn_update_dpp(b, b, decltype(c)::value, decltype(r)::value, 0xf, false)), v);
+  });
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
 
 __device__ __forceinline__ void sample_clear(SampleLds& s) {
 #pragma unroll
@@ -226,37 +272,26 @@ __device__ __forceinline__ void sample_clear(SampleLds& s) {
 // The first bin with which the counts reach `count` or the weights `weight` (u >= 0: the first whose running weight is above u
 // times the whole). All threads, after their additions to the bins.
 __device__ __forceinline__ SampleFound sample_find(SampleLds& s, uint32_t count, uint64_t weight, double u = -1.0) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = 2 * threadIdx.x;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), b = 2 * threadIdx.x;
   __syncthreads();
   if (threadIdx.x == 0) s.found.bin = -1;
   const uint32_t c0 = s.count[b], c1 = s.count[b + 1];
   const uint64_t w0 = s.weight[b], w1 = s.weight[b + 1];
-  uint32_t c = c0 + c1;
-  uint64_t w = w0 + w1;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t cb = __shfl_up(c, o);
-    const uint64_t wb = __shfl_up((unsigned long long)w, o);
-    if (lane >= o) {
-      c += cb;
-      w += wb;
-    }
-  }
+  uint32_t c = wave_scan(c0 + c1);
+  uint64_t w = wave_scan(w0 + w1);
   if (lane == 63) {
     s.wave_count[wave] = c;
     s.wave_weight[wave] = w;
   }
   __syncthreads();
-  uint32_t all_c = 0;
-  uint64_t all_w = 0;
-#pragma unroll
-  for (int k = 0; k < kSampleThreads / 64; ++k) {
-    if (k == wave) {
-      c += all_c;
-      w += all_w;
-    }
-    all_c += s.wave_count[k];
-    all_w += s.wave_weight[k];
+  // The sums of the waves before, and of all, from 16 lanes' scan.
+  const uint32_t upto_c = row_scan(s.wave_count[lane & 15]);
+  const uint64_t upto_w = row_scan(s.wave_weight[lane & 15]);
+  const uint32_t all_c = lane_of(upto_c, 15);
+  const uint64_t all_w = lane_of(upto_w, 15);
+  if (wave > 0) {
+    c += lane_of(upto_c, wave - 1);
+    w += lane_of(upto_w, wave - 1);
   }
   if (u >= 0.0) {
     weight = (uint64_t)(fmin(u, 1.0) * (double)all_w) + 1;
@@ -278,17 +313,6 @@ __device__ __forceinline__ SampleFound sample_find(SampleLds& s, uint32_t count,
   f.all = all_c;
   f.weight_all = all_w;
   return f;
-}
-
-__device__ __forceinline__ float sample_block_max(float v, SampleLds& s) {
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) v = max_or_nan(__shfl_xor(v, o), v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s.wave_max[threadIdx.x >> 6] = v;
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < kSampleThreads / 64; ++k) v = max_or_nan(s.wave_max[k], v);
-  return v;
 }
 
 // Bits by which a span of values is shifted to fall into the bins.
@@ -316,10 +340,22 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
     s.actives = s.listed = 0;
     s.lowest = ~0u;
   }
-  float top = maxima[0];
+  // The largest, and the least above -inf.
+  float top = -INFINITY, least = INFINITY;
 #pragma unroll
-  for (int k = 1; k < kEach; ++k) top = max_or_nan(maxima[k], top);
-  top = sample_block_max(top, s);
+  for (int k = 0; k < kEach; ++k) {
+    top = max_or_nan(maxima[k], top);
+    if (maxima[k] > -INFINITY) least = fminf(least, maxima[k]);
+  }
+  top = wave_max(top);
+  least = -wave_max(-least);
+  if ((tid & 63) == 0) {
+    s.wave_max[tid >> 6] = top;
+    s.wave_least[tid >> 6] = least;
+  }
+  __syncthreads();
+  top = wave_max(s.wave_max[tid & 15]);
+  least = -wave_max(-s.wave_least[tid & 15]);
   auto answer = [&](int64_t token, float logprob) {
     if (tid == 0) {
       a.tokens[i] = token;
@@ -329,13 +365,17 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
   // A NaN among the logits or for u, or nothing above -inf.
   if (!(top > -INFINITY) || u != u) return answer(-1, __builtin_nanf(""));
 
-  // The logits of a range of places, by single loads.
+  // The logits of a range of places, by single loads, four requested at once.
+  constexpr uint32_t kAtOnce = 4;
   auto range = [&](uint32_t lo, uint32_t n, auto f) {
-    for (uint32_t k = tid; k < n; k += kSampleThreads)
-      if (lo + k < (uint32_t)a.V) {
-        const float z = to_f32(row[lo + k]);
-        f(Key::of(z), z, lo + k);
-      }
+    for (uint32_t k = tid; k < n; k += kAtOnce * kSampleThreads) {
+      float z[kAtOnce];
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) z[q] = to_f32(row[min(lo + k + q * kSampleThreads, (uint32_t)a.V - 1)]);
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q)
+        if (k + q * kSampleThreads < n && lo + k + q * kSampleThreads < (uint32_t)a.V) f(Key::of(z[q]), z[q], lo + k + q * kSampleThreads);
+    }
   };
 
   if (set.greedy) {
@@ -429,26 +469,29 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
   uint32_t listed = 0;
   // The logits of the active groups that are not below the bound: eight lanes a group, four groups requested at once.
   auto stream = [&](auto f) {
-    constexpr int kAhead = 4, kAtOnce = kSampleThreads / 8;
-    for (int k0 = tid / 8; k0 < actives; k0 += kAhead * kAtOnce) {
+    constexpr int kAhead = 4, kGroups = kSampleThreads / 8;
+    for (int k0 = tid / 8; k0 < actives; k0 += kAhead * kGroups) {
 #pragma unroll
       for (int r = 0; r < REP; ++r) {
         RawRow<T> raw[kAhead];
         int at[kAhead];
 #pragma unroll
         for (int q = 0; q < kAhead; ++q) {
-          at[q] = (int)s.active[min(k0 + q * kAtOnce, actives - 1)] * kGroup + r * 64 + (tid % 8) * kNormVec;
+          at[q] = (int)s.active[min(k0 + q * kGroups, actives - 1)] * kGroup + r * 64 + (tid % 8) * kNormVec;
           raw[q].clear();
           load_raw<END>(row + at[q], a.V - at[q], raw[q]);
         }
 #pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-          const int n = k0 + q * kAtOnce < actives ? a.V - at[q] : 0;
-          align_end<END>(a.V - at[q], raw[q]);
+        for (int q = 0; q < kAhead; ++q) align_end<END>(a.V - at[q], raw[q]);
+        // One after the other out of the registers' front: unrolled, these loops are 100 KB of code that a single row
+        // waits for.
+#pragma nounroll
+        for (int e = 0; e < kNormVec; ++e) {
 #pragma unroll
-          for (int e = 0; e < kNormVec; ++e) {
-            const float z = raw[q].at(e);
-            if (e < n && z >= bound) f(Key::of(z), z, (uint32_t)(at[q] + e));
+          for (int q = 0; q < kAhead; ++q) {
+            const float z = raw[q].at(0);
+            if (k0 + q * kGroups < actives && at[q] + e < a.V && z >= bound) f(Key::of(z), z, (uint32_t)(at[q] + e));
+            raw[q].drop(1);
           }
         }
       }
@@ -488,27 +531,15 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
   auto find_bound = [&]() {
     bound = -INFINITY;
     if (set.by_k && set.k <= a.groups && top < INFINITY) {
-      // The k-th largest of the groups' maxima: k logits at least are as large.
-      float least = INFINITY;
-#pragma unroll
-      for (int k = 0; k < kEach; ++k)
-        if (maxima[k] > -INFINITY) least = fminf(least, maxima[k]);
-      least = -sample_block_max(-least, s);
+      // The k-th largest of the groups' maxima: k logits at least are as large. It is no smaller than the end of its bin.
       const float inv = top > least ? (float)(kSampleBins - 1) / (top - least) : 0.f;
       if (inv < INFINITY && top - least < INFINITY) {
-        auto bin = [&](float m) { return min((int)((top - m) * inv), kSampleBins - 1); };
         sample_clear(s);
 #pragma unroll
         for (int k = 0; k < kEach; ++k)
-          if (maxima[k] > -INFINITY) atomicAdd(&s.count[bin(maxima[k])], 1u);
+          if (maxima[k] > -INFINITY) atomicAdd(&s.count[min((int)((top - maxima[k]) * inv), kSampleBins - 1)], 1u);
         const SampleFound f = sample_find(s, (uint32_t)set.k, ~0ull);
-        if (f.bin >= 0) {
-          float lowest = INFINITY;
-#pragma unroll
-          for (int k = 0; k < kEach; ++k)
-            if (maxima[k] > -INFINITY && bin(maxima[k]) <= f.bin) lowest = fminf(lowest, maxima[k]);
-          bound = -sample_block_max(-lowest, s);
-        }
+        if (f.bin >= 0) bound = inv > 0.f ? top - ((float)(f.bin + 1) / inv * (1.f + 0x1p-20f) + fabsf(top) * 0x1p-22f) : top;
       }
     }
     if (set.by_least && !(set.by_k && set.by_p)) bound = fmaxf(bound, bound_of((double)set.least));
@@ -533,6 +564,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
     uint64_t before = 0;
     uint32_t ahead = 0;
     if (mine)
+#pragma unroll 4
       for (uint32_t k = 0; k < listed; ++k) {
         const bool first = rank(s.list_key[k], s.list_at[k]) > order;
         before += first ? s.weight[k] : 0;
@@ -547,6 +579,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
     __syncthreads();
     if (!kept) return;
     uint64_t up_to = 0, all = 0;
+#pragma unroll 4
     for (uint32_t k = 0; k < listed; ++k) {
       up_to += s.list_at[k] <= at ? s.weight[k] : 0;
       all += s.weight[k];
