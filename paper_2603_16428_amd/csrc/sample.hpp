@@ -210,7 +210,7 @@ struct SampleLds {
   uint32_t wave_count[16];
   float wave_max[16], wave_least[16];
   uint32_t actives, listed, lowest;
-  unsigned long long kept;
+  unsigned long long kept, all;
   SampleFound found;
 };
 
@@ -399,34 +399,6 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
   const double one = __builtin_ldexp(1.0, a.bits);
   // A weight in fixed point: below 2^52, so that adding 2^52 rounds it to an integer in the low bits.
   auto fixed = [&](double w) { return __builtin_bit_cast(uint64_t, fma(w, one, 0x1p52)) - __builtin_bit_cast(uint64_t, 0x1p52); };
-  // The token whose running sum of `weight_of` (key, logit, place) passes u times the whole, of places lo .. lo + n - 1, which
-  // `each` goes through. Its place, and the whole.
-  auto draw = [&](uint32_t lo, uint32_t n, double part, auto each, auto weight_of, uint64_t& whole) {
-    uint64_t target = 0;
-    for (bool first = true;; first = false) {
-      const int shift = sample_shift(n - 1);
-      sample_clear(s);
-      auto add = [&](uint32_t key, float z, uint32_t at) {
-        if (at - lo >= n) return;
-        const uint64_t w = weight_of(key, z, at);
-        if (w != 0) atomicAdd(&s.weight[(at - lo) >> shift], (unsigned long long)w);
-      };
-      if (first) each(add);
-      else if (n <= (uint32_t)kGroup * kPartGroups) range(lo, n, add);
-      else each(add);
-      const SampleFound f = first ? sample_find(s, ~0u, 0, part) : sample_find(s, ~0u, target);
-      if (first) {
-        whole = f.weight_all;
-        target = (uint64_t)(fmin(part, 1.0) * (double)whole) + 1;
-        target = target > whole ? whole : target;
-      }
-      if (f.bin < 0) return lo;  // (no weight at all, which the kept ones' largest rules out)
-      target -= f.weight_before;
-      lo += (uint32_t)f.bin << shift;
-      n = min(n - ((uint32_t)f.bin << shift), 1u << shift);
-      if (shift == 0) return lo;
-    }
-  };
   auto logprob = [&](uint32_t at, double sum) {
     const float z = to_f32(row[at]);
     return (float)((z == top ? 0.0 : ((double)z - (double)top) / (double)set.T) - log(sum));
@@ -437,18 +409,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
   auto rank = [](uint32_t key, uint32_t at) { return (uint64_t)key << 32 | (0xffffffffu - at); };
   uint64_t cut = 0;
   int cell = -1;  // the listed logits' cell, the last of which some are kept (-1: no cell)
-  // The token of the part in which the running weight of the parts passes `chance`, relative to the part's own maximum.
-  auto draw_in = [&](const SampleFound& f) {
-    const float of = a.part_max[i * a.parts + f.bin];
-    const double inside = (fmin(chance, 1.0) * (double)f.weight_all - (double)f.weight_before) / (double)f.weight;
-    const uint32_t lo = (uint32_t)f.bin * kPartGroups * kGroup, n = min((uint32_t)(kPartGroups * kGroup), (uint32_t)a.V - lo);
-    uint64_t whole;
-    const uint32_t at = draw(lo, n, fmin(fmax(inside, 0.0), 1.0), [&](auto add) { range(lo, n, add); }, [&](uint32_t key, float z, uint32_t place) {
-      return rank(key, place) < cut || (cell >= 0 && sample_cell(z, top, set.rate) > cell) ? (uint64_t)0 : fixed(sample_weight(z, of, set.rate, s.table));
-    }, whole);
-    answer(at, logprob(at, (double)f.weight_all / one));
-  };
-
+  // Where the token is known to lie: the part in which the parts' running weight passes `chance`.
+  SampleFound part;
+  part.bin = -1;
   // The whole row's weight from its parts'.
   double sum = 0.0;
   if (set.sums()) {
@@ -457,9 +420,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
       const double w = a.part_sum[i * a.parts + tid] * sample_weight(a.part_max[i * a.parts + tid], top, set.rate, s.table);
       s.weight[tid] = (uint64_t)(w * one + 0.5);
     }
-    const SampleFound f = sample_find(s, ~0u, 0, chance);
-    sum = (double)f.weight_all / one;
-    if (set.whole()) return draw_in(f);
+    part = sample_find(s, ~0u, 0, chance);
+    sum = (double)part.weight_all / one;
+    if (!set.whole()) part.bin = -1;
   }
 
   auto weight = [&](float z) { return sample_weight(z, top, set.rate, s.table); };
@@ -552,41 +515,53 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
     return target >= 1.0 ? (uint64_t)target : (uint64_t)1;
   };
 
-  // Few logits (a thread each): every one looks at all others.
+  // Few logits: every one looks at all others, whose number is shared out among as many threads as there are.
   auto few = [&]() {
-    const bool mine = tid < (int)listed;
-    const uint32_t key = mine ? s.list_key[tid] : 0u, at = mine ? s.list_at[tid] : ~0u;
+    int slots = 64;
+    while (slots < (int)listed) slots *= 2;
+    const int me = tid % slots, segment = tid / slots, segments = kSampleThreads / slots;
+    const bool mine = me < (int)listed;
+    unsigned long long *w_of = s.weight, *before_of = w_of + kSampleFew, *kept_of = before_of + kSampleFew, *up_to_of = kept_of + kSampleFew;
+    const uint32_t key = mine ? s.list_key[me] : 0u, at = mine ? s.list_at[me] : ~0u;
     const double share = mine ? weight(Key::value(key)) : 0.0;
     const uint64_t w = fixed(share), order = rank(key, at);
-    if (mine) s.weight[tid] = w;
-    if (tid == 0) s.kept = 0;
+    if (segment == 0) {
+      w_of[me] = mine ? w : 0;
+      before_of[me] = up_to_of[me] = 0;
+      s.count[me] = 0;
+    }
+    if (tid == 0) s.kept = s.all = 0;
     __syncthreads();
     uint64_t before = 0;
     uint32_t ahead = 0;
-    if (mine)
-#pragma unroll 4
-      for (uint32_t k = 0; k < listed; ++k) {
-        const bool first = rank(s.list_key[k], s.list_at[k]) > order;
-        before += first ? s.weight[k] : 0;
-        ahead += first;
-      }
-    bool kept = mine && (!set.by_k || ahead < (uint32_t)set.k);
-    if (kept && w != 0) atomicAdd(&s.kept, (unsigned long long)w);
-    __syncthreads();
-    if (set.by_p) kept = kept && before < share_of(set.by_k ? (double)s.kept : sum * one);
-    if (set.by_least) kept = kept && share >= (double)set.least;
-    if (mine) s.weight[tid] = kept ? w : 0;
-    __syncthreads();
-    if (!kept) return;
-    uint64_t up_to = 0, all = 0;
-#pragma unroll 4
-    for (uint32_t k = 0; k < listed; ++k) {
-      up_to += s.list_at[k] <= at ? s.weight[k] : 0;
-      all += s.weight[k];
+    for (int k = segment; k < (int)listed; k += segments) {
+      const bool first = rank(s.list_key[k], s.list_at[k]) > order;
+      before += first ? w_of[k] : 0;
+      ahead += first;
     }
+    if (mine) {
+      atomicAdd(&before_of[me], (unsigned long long)before);
+      atomicAdd(&s.count[me], ahead);
+    }
+    __syncthreads();
+    bool kept = mine && (!set.by_k || s.count[me] < (uint32_t)set.k);
+    if (kept && segment == 0) atomicAdd(&s.kept, (unsigned long long)w);
+    __syncthreads();
+    if (set.by_p) kept = kept && before_of[me] < share_of(set.by_k ? (double)s.kept : sum * one);
+    if (set.by_least) kept = kept && share >= (double)set.least;
+    if (segment == 0) {
+      kept_of[me] = kept ? w : 0;
+      if (kept) atomicAdd(&s.all, (unsigned long long)w);
+    }
+    __syncthreads();
+    uint64_t up_to = 0;
+    for (int k = segment; k < (int)listed; k += segments) up_to += s.list_at[k] <= at ? kept_of[k] : 0;
+    if (kept) atomicAdd(&up_to_of[me], (unsigned long long)up_to);
+    __syncthreads();
+    const uint64_t all = s.all;
     uint64_t target = (uint64_t)(fmin(chance, 1.0) * (double)all) + 1;
     target = target > all ? all : target;
-    if (up_to >= target && up_to - w < target) {
+    if (kept && segment == 0 && up_to_of[me] >= target && up_to_of[me] - w < target) {
       a.tokens[i] = at;
       if (a.logprobs != nullptr) a.logprobs[i] = logprob(at, (double)all / one);
     }
@@ -657,14 +632,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
   bool by_cells = set.cells, ready = false;
   const double of_row = sum;
 #pragma nounroll
-  for (int what = 0; what < 3; ++what) {  // top-k, then top-p
-    if (!by_cells && !ready) {
-      find_bound();
-      list();
-      ready = true;
-      if (listed <= (uint32_t)kSampleFew) return few();
-    }
-    if (what == 0 ? !set.by_k : what == 1 ? !set.by_p : true) continue;
+  for (int what = set.whole() ? 3 : 0; what < 3; ++what) {  // top-k, then top-p
+    const bool wanted = what == 0 ? set.by_k : what == 1 && set.by_p;
+    if (!wanted && (by_cells || ready)) continue;
     const uint32_t count = what == 0 ? (uint32_t)set.k : ~0u;
     const uint64_t target = what == 0 ? ~0ull : share_of(sum * one);
     uint32_t before = 0;
@@ -682,37 +652,70 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
       cell = f.bin;
       const double c = set.rate * (4.0 / (256.0 * 1.4426950408889634074));
       bound = top < INFINITY ? below((floor((double)top * c) - cell) / c) : top;
-      list();
-      if (listed > (uint32_t)kSampleList) {  // too many logits in one cell: the long way
-        by_cells = false;
-        cell = -1;
-        cut = 0;
-        sum = of_row;
-        what = -1;
-        continue;
-      }
+    } else if (!ready) {
+      find_bound();
     }
+    if (by_cells || !ready) list();
+    if (by_cells && listed > (uint32_t)kSampleList) {  // too many logits in one cell: the long way
+      by_cells = false;
+      cell = -1;
+      cut = 0;
+      sum = of_row;
+      what = -1;
+      continue;
+    }
+    if (!by_cells && !ready && listed <= (uint32_t)kSampleFew) return few();
+    ready = true;
+    if (!wanted) continue;
     const uint64_t kept = keep(count, target, before, weight_before);
     if (what == 0) sum = (double)kept / one;
   }
   if (by_cells) {
     sample_clear(s);
-    tables([&](int part, int c, uint32_t, uint64_t w) {
-      if (cell < 0 || c < cell) atomicAdd(&s.weight[part], (unsigned long long)w);
+    tables([&](int of, int c, uint32_t, uint64_t w) {
+      if (cell < 0 || c < cell) atomicAdd(&s.weight[of], (unsigned long long)w);
     });
     if (cell >= 0)
-      each([&](uint32_t key, float z, uint32_t at) {
-        if (rank(key, at) >= cut) atomicAdd(&s.weight[at / (kPartGroups * kGroup)], (unsigned long long)fixed(weight(z)));
-      });
-    return draw_in(sample_find(s, ~0u, 0, chance));
+      for (uint32_t k = tid; k < listed; k += kSampleThreads)
+        if (rank(s.list_key[k], s.list_at[k]) >= cut)
+          atomicAdd(&s.weight[s.list_at[k] / (kPartGroups * kGroup)], (unsigned long long)fixed(weight(Key::value(s.list_key[k]))));
+    part = sample_find(s, ~0u, 0, chance);
   }
-  uint64_t whole;
-  const uint32_t at = draw(0, (uint32_t)a.V, chance, each, [&](uint32_t key, float z, uint32_t place) {
-    if (z < bound || rank(key, place) < cut) return (uint64_t)0;
-    const double w = weight(z);
-    return set.by_least && w < (double)set.least ? (uint64_t)0 : fixed(w);
-  }, whole);
-  answer(at, logprob(at, (double)whole / one));
+
+  // The token of all kept ones, or of a part's (in weights relative to the part's own maximum): where the running weight by places passes
+  // `share` times the whole; again inside the bin that it lies in, until that is one place.
+  const bool inside = part.bin >= 0;
+  const float of = inside ? a.part_max[i * a.parts + part.bin] : top;
+  uint32_t lo = inside ? (uint32_t)part.bin * kPartGroups * kGroup : 0u;
+  uint32_t n = inside ? min((uint32_t)(kPartGroups * kGroup), (uint32_t)a.V - lo) : (uint32_t)a.V;
+  double share = fmin(chance, 1.0);
+  if (inside) share = fmin(fmax((share * (double)part.weight_all - (double)part.weight_before) / (double)part.weight, 0.0), 1.0);
+  uint64_t target = 0, whole = part.weight_all;
+  bool first = true;
+#pragma nounroll
+  for (int shift = 1; shift > 0; first = false) {
+    shift = sample_shift(n - 1);
+    sample_clear(s);
+    auto add = [&](uint32_t key, float z, uint32_t place) {
+      if (place - lo >= n || z < bound || rank(key, place) < cut || (cell >= 0 && sample_cell(z, top, set.rate) > cell)) return;
+      if (set.by_least && weight(z) < (double)set.least) return;
+      const uint64_t w = fixed(sample_weight(z, of, set.rate, s.table));
+      if (w != 0) atomicAdd(&s.weight[(place - lo) >> shift], (unsigned long long)w);
+    };
+    if (first && !inside) each(add);
+    else range(lo, n, add);
+    const SampleFound f = sample_find(s, ~0u, target, first ? share : -1.0);
+    if (first) {
+      target = (uint64_t)(share * (double)f.weight_all) + 1;
+      target = target > f.weight_all ? f.weight_all : target;
+      if (!inside) whole = f.weight_all;
+    }
+    if (f.bin < 0) break;  // (no weight at all, which the kept ones' largest rules out)
+    target -= f.weight_before;
+    lo += (uint32_t)f.bin << shift;
+    n = min(n - ((uint32_t)f.bin << shift), 1u << shift);
+  }
+  answer(lo, logprob(lo, (double)whole / one));
 }
 
 }  // namespace lce
