@@ -79,7 +79,7 @@ lce_status_t lce_mxfp4_matmul(const void* x_codes, const void* x_scales, int64_t
  *   top_p  of these, the ones whose predecessors weigh less than top_p of these together (1 or more: all; the first always),
  *   min_p  of these, the ones with w_v >= min_p (0 or less: all; 1 at most).
  * token = the first kept v for which the sum of kept w up to and with v, by rising v, is above u times the sum of all kept.
- * A temperature that is not above 0 takes the largest logit's first place. A row with a NaN, or nothing above -inf, or whose u is NaN, gives
+ * A temperature that is not above 0 takes the largest logit's first place (above 1e30: as 1e30). A row with a NaN, or nothing above -inf, or whose u is NaN, gives
  * -1; u below 0 counts as 0, from 1 on the last kept token comes. +inf are the largest and equal. Weights are computed in 64 bits and
  * added in integers (a 2^42nd of the largest weight, or less): a token's smaller weight counts as none, and a result does
  * not depend on the order of additions.

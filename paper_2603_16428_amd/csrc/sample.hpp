@@ -52,6 +52,7 @@ struct SampleRow {
 __device__ __forceinline__ SampleRow sample_row(const SampleArgs& a, int64_t i) {
   SampleRow r;
   r.T = a.temperatures ? a.temperatures[i] : a.temperature;
+  r.T = r.T > 1e30f ? 1e30f : r.T;  // (all weights are equal then, and no product below is 0 times infinity)
   r.p = a.top_ps ? a.top_ps[i] : a.top_p;
   r.least = fminf(a.min_ps ? a.min_ps[i] : a.min_p, 1.f);  // the largest is always kept
   r.k = a.top_ks ? a.top_ks[i] : a.top_k;

@@ -127,6 +127,12 @@ def test_gradient_of_few_or_all_tokens(lce, kind):
     assert torch.equal(kept, got)
 
 
+def test_very_wide_rows(lce):
+    tokens, weight, grad = _inputs(70, 70005, 3, "bf16")
+    _check_rows(lce.embedding_forward(tokens, weight, 2.0), tokens, weight, 2.0)
+    _check_gradient(lce.embedding_backward(grad, tokens, 3), grad, tokens, 3)
+
+
 def test_long_sums(lce):
     """A token at 300000 positions: a chain of fp32 additions would lose all that is added after the first."""
     N = 300000

@@ -132,6 +132,15 @@ def test_temperatures_of_any_size(lce):
             _check(lce, z, u, temperature=t, **s)
 
 
+def test_infinite_temperature(lce):
+    """All logits above -inf become equal."""
+    z, u = _logits(5, 2000, "fp32", 1.0)
+    z[:, ::3] = -math.inf
+    for s in (dict(), dict(top_k=10), dict(top_p=0.5), dict(min_p=1.0), dict(top_k=1900, top_p=0.5)):
+        _check(lce, z, u, temperature=1e30, **s)
+        assert torch.equal(lce.sample(z, u, temperature=math.inf, **s), lce.sample(z, u, temperature=1e30, **s))
+
+
 def test_settings_of_each_row(lce):
     N, V = 64, 5000
     g = torch.Generator().manual_seed(8)
