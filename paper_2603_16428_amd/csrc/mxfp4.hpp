@@ -383,21 +383,28 @@ __global__ __launch_bounds__(512) void mxfp4_many_kernel(const MxMatmulArgs a) {
     for (int i = 0; i < kI; ++i) sw[i] = *lds_at<uint16_t>(addr_sw + slot + i * 16 * kMxStepGroups);
 #pragma unroll
     for (int j = 0; j < kJ; ++j) sx[j] = *lds_at<uint16_t>(addr_sx + slot + j * 16 * kMxStepGroups);
-    auto half = [&](auto h) {
+    u32x4 w[2][kI], x[2][kJ];
+    // (the pieces' permutation flips bits 4 to 6; group 2 quarter + 1 is group 2 quarter's bit 4 flipped)
+    auto fragments = [&](auto h) {
       constexpr int kH = decltype(h)::value;
-      u32x4 w[kI], x[kJ];
-      // (the pieces' permutation flips bits 4 to 6; group 2 quarter + 1 is group 2 quarter's bit 4 flipped)
 #pragma unroll
-      for (int i = 0; i < kI; ++i) w[i] = *lds_at<u32x4>(((addr_w + slot) ^ (16u * kH)) + i * 16 * kMxStepBytes);
+      for (int i = 0; i < kI; ++i) w[kH][i] = *lds_at<u32x4>(((addr_w + slot) ^ (16u * kH)) + i * 16 * kMxStepBytes);
 #pragma unroll
-      for (int j = 0; j < kJ; ++j) x[j] = *lds_at<u32x4>(((addr_x + slot) ^ (16u * kH)) + j * 16 * kMxStepBytes);
+      for (int j = 0; j < kJ; ++j) x[kH][j] = *lds_at<u32x4>(((addr_x + slot) ^ (16u * kH)) + j * 16 * kMxStepBytes);
+    };
+    auto multiply = [&](auto h) {
+      constexpr int kH = decltype(h)::value;
 #pragma unroll
       for (int j = 0; j < kJ; ++j)
 #pragma unroll
-        for (int i = 0; i < kI; ++i) acc[i][j] = mx_mfma<kH>(w[i], sw[i], x[j], sx[j], acc[i][j]);
+        for (int i = 0; i < kI; ++i) acc[i][j] = mx_mfma<kH>(w[kH][i], sw[i], x[kH][j], sx[j], acc[i][j]);
     };
-    half(std::integral_constant<int, 0>{});
-    half(std::integral_constant<int, 1>{});
+    using std::integral_constant;
+    fragments(integral_constant<int, 0>{});
+    fragments(integral_constant<int, 1>{});
+    __builtin_amdgcn_sched_barrier(0);
+    multiply(integral_constant<int, 0>{});
+    multiply(integral_constant<int, 1>{});
   }
   // Element r of block (i, j): v = 16 i + 4 quarter + r, m = 16 j + row of the wave's part.
 #pragma unroll
