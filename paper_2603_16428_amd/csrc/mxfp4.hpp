@@ -301,13 +301,16 @@ __global__ __launch_bounds__(256, 2) void mxfp4_few_kernel(const MxMatmulArgs a)
   }
 }
 
-// Many rows: a tile of 256 rows of W by BN of x for eight waves (4 x 2), each 64 by BN / 2 in 16 x 16 blocks. A step is 256
+// Many rows: a tile of 256 rows of W by BN of x for WAVES waves in two columns, each with 16 x 16 blocks of its part (BN 256: eight
+// waves, 64 x 128; four of 128 x 128 read less from LDS but have nothing to run under their waits, 924 us against 733 for
+// 2048 x 3584 x 152064; BN 128: four waves, 128 x 64, 89 us against 91 with eight for 128 x 4096 x 128256). A step is 256
 // values of K, 128 bytes of a row: whole cache lines, LDS-DMA loads of 8 rows each into one of two slots. The 16-byte
 // pieces of LDS row r are permuted by r % 8, so that a fragment's 16 rows lie in distinct banks. The scales go through
-// registers, since their rows may begin at any byte.
-template <typename T, int BN>
-__global__ __launch_bounds__(512) void mxfp4_many_kernel(const MxMatmulArgs a) {
-  constexpr int kBM = 256, kI = 4, kJ = BN / 32, kWaves = 8;
+// registers, since their rows may begin at any byte. Bound by LDS: what a step's fragments read and its loads write takes as
+// long as its products at the full rate. 2048 x 3584 x 152064: 3.0 PFLOP/s, 4096 x 8192 x 32000: 3.5.
+template <typename T, int BN, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void mxfp4_many_kernel(const MxMatmulArgs a) {
+  constexpr int kBM = 256, kWaves = WAVES, kWavesV = WAVES / 2, kI = kBM / kWavesV / 16, kJ = BN / 32, kThreads = 64 * WAVES;
   constexpr int kW = kBM * kMxStepBytes, kX = BN * kMxStepBytes, kSw = kBM * kMxStepGroups, kSx = BN * kMxStepGroups;
   constexpr int kSlot = kW + kX + kSw + kSx;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
@@ -339,36 +342,47 @@ __global__ __launch_bounds__(512) void mxfp4_many_kernel(const MxMatmulArgs a) {
       dma16(rsrc_x, to + kW + b * 1024, in ? row_off + piece + k + (uint32_t)(8 * b) * pitch : kOOB);
     }
   };
-  // Thread t has the scales of W's row t, then of x's row t - 256.
-  const bool of_w = threadIdx.x < kBM;
-  const int srow = of_w ? min((int)threadIdx.x, rows_w - 1) : min((int)threadIdx.x - kBM, rows_x - 1);
-  const uint8_t* ps = of_w ? a.w_scales + (v0 + srow) * groups : a.x_scales + (m0 + srow) * groups;
-  const bool has_scales = threadIdx.x < kBM + BN;
-  auto load_scales = [&](int step) {
-    uint64_t s = 0x7f7f7f7f7f7f7f7full;
+  // A thread has the scales of one row or two: of W's rows, then of x's.
+  constexpr int kScaleRows = (kBM + BN + kThreads - 1) / kThreads;
+  const uint8_t* ps[kScaleRows];
+#pragma unroll
+  for (int k = 0; k < kScaleRows; ++k) {
+    const int r = k * kThreads + (int)threadIdx.x;
+    ps[k] = r < kBM ? a.w_scales + (v0 + min(r, rows_w - 1)) * groups : a.x_scales + (m0 + min(r - kBM, rows_x - 1)) * groups;
+  }
+  auto has_scales = [&](int k) { return (k + 1) * kThreads <= kBM + BN || k * kThreads + (int)threadIdx.x < kBM + BN; };
+  auto load_scales = [&](int step, uint64_t (&s)[kScaleRows]) {
     const uint32_t g = (uint32_t)step * kMxStepGroups;
-    if (!has_scales || step >= steps) return s;
-    if (g + kMxStepGroups <= groups) {
-      __builtin_memcpy(&s, ps + g, 8);
-    } else {
-      for (uint32_t k = g; k < groups; ++k) s = (s & ~(0xffull << (8 * (k - g)))) | (uint64_t)ps[k] << (8 * (k - g));
+#pragma unroll
+    for (int k = 0; k < kScaleRows; ++k) {
+      s[k] = 0x7f7f7f7f7f7f7f7full;
+      if (!has_scales(k) || step >= steps) continue;
+      if (g + kMxStepGroups <= groups) {
+        __builtin_memcpy(&s[k], ps[k] + g, 8);
+      } else {
+        for (uint32_t j = g; j < groups; ++j) s[k] = (s[k] & ~(0xffull << (8 * (j - g)))) | (uint64_t)ps[k][j] << (8 * (j - g));
+      }
     }
-    return s;
   };
-  auto put_scales = [&](int slot, uint64_t s) {
-    if (has_scales) *(uint64_t*)(smem + slot * kSlot + kW + kX + threadIdx.x * 8) = s;
+  auto put_scales = [&](int slot, const uint64_t (&s)[kScaleRows]) {
+#pragma unroll
+    for (int k = 0; k < kScaleRows; ++k)
+      if (has_scales(k)) *(uint64_t*)(smem + slot * kSlot + kW + kX + (k * kThreads + threadIdx.x) * 8) = s[k];
   };
   f32x4 acc[kI][kJ] = {};
-  const int wv = wave & 3, wm = wave >> 2;
+  constexpr int kRowsV = kBM / kWavesV;  // of a wave
+  const int wv = wave % kWavesV, wm = wave / kWavesV;
   // Fragment of block b (16 rows), group pair half j: piece 2 quarter + j of row 16 b + row.
   const uint32_t frag0 = (uint32_t)(row * kMxStepBytes) + (uint32_t)(((2 * quarter) ^ (row & 7)) * 16);
-  const uint32_t addr_w = base + (uint32_t)(wv * 64 * kMxStepBytes) + frag0;
+  const uint32_t addr_w = base + (uint32_t)(wv * kRowsV * kMxStepBytes) + frag0;
   const uint32_t addr_x = base + kW + (uint32_t)(wm * (BN / 2) * kMxStepBytes) + frag0;
-  const uint32_t addr_sw = base + kW + kX + (uint32_t)((wv * 64 + row) * kMxStepGroups + 2 * quarter);
+  const uint32_t addr_sw = base + kW + kX + (uint32_t)((wv * kRowsV + row) * kMxStepGroups + 2 * quarter);
   const uint32_t addr_sx = base + kW + kX + kSw + (uint32_t)((wm * (BN / 2) + row) * kMxStepGroups + 2 * quarter);
+  uint64_t next[kScaleRows];
   dma(0, 0);
-  put_scales(0, load_scales(0));
-  uint64_t next = load_scales(1);
+  load_scales(0, next);
+  put_scales(0, next);
+  load_scales(1, next);
   for (int t = 0; t < steps; ++t) {
     const uint32_t slot = (uint32_t)(t & 1) * kSlot;
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -376,7 +390,7 @@ __global__ __launch_bounds__(512) void mxfp4_many_kernel(const MxMatmulArgs a) {
     if (t + 1 < steps) {
       dma(t + 1, (t + 1) & 1);
       put_scales((t + 1) & 1, next);
-      next = load_scales(t + 2);
+      load_scales(t + 2, next);
     }
     uint32_t sw[kI], sx[kJ];
 #pragma unroll
@@ -413,7 +427,7 @@ __global__ __launch_bounds__(512) void mxfp4_many_kernel(const MxMatmulArgs a) {
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int i = 0; i < kI; i += 2) {
-        const int64_t v = v0 + wv * 64 + 16 * i + 8 * quarter;
+        const int64_t v = v0 + wv * kRowsV + 16 * i + 8 * quarter;
         const u32x4 y = regroup16<T>(acc[i][j], acc[i + 1][j]);
         T* p = (T*)a.out + m * a.out_ld + v;
         if (m >= a.M) continue;
@@ -430,7 +444,7 @@ __global__ __launch_bounds__(512) void mxfp4_many_kernel(const MxMatmulArgs a) {
     } else {
 #pragma unroll
       for (int i = 0; i < kI; ++i) {
-        const int64_t v = v0 + wv * 64 + 16 * i + 4 * quarter;
+        const int64_t v = v0 + wv * kRowsV + 16 * i + 4 * quarter;
         T* p = (T*)a.out + m * a.out_ld + v;
         if (m >= a.M) continue;
         if (v + 4 <= a.V) {

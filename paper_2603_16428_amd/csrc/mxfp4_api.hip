@@ -33,18 +33,22 @@ lce_status_t run_mxfp4_many(MxMatmulArgs a, hipStream_t s) {
   a.tiles_v = (int)cdiv(a.V, 256);
   const int64_t tiles = (int64_t)a.tiles_m * a.tiles_v;
   if (tiles > (1 << 22)) return LCE_ERR_UNSUPPORTED;
-  auto kernel = mxfp4_many_kernel<T, BN>;
+  constexpr int kWaves = BN / 32;
+  auto kernel = mxfp4_many_kernel<T, BN, kWaves>;
   constexpr int kSmem = mx_many_smem<BN>();
   if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kSmem) != hipSuccess) return LCE_ERR_HIP;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(512), kSmem, s, a);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(64 * kWaves), kSmem, s, a);
   return launched();
 }
 
 template <typename T>
 lce_status_t run_mxfp4_matmul(const MxMatmulArgs& a, hipStream_t s) {
   // Few rows read W straight into registers. From 49 on the tile of 128 is the faster (4096 x 128256: 48 rows 76 us, 64 rows
-  // 89 us so and 85 in the tile, which takes 90 for 128).
-  if (a.M > 48) return a.M <= 128 ? run_mxfp4_many<T, 128>(a, s) : run_mxfp4_many<T, 256>(a, s);
+  // 89 us so and 86 in the tile, which takes 89 for 128).
+  // More rows than that take the tile of 256 (256 rows: 107 us against 152, 2048: 686 against 1168) where it leaves no more than half of
+  // the 256 CUs without one (2048 x 1024 x 2048: 14 us, 11 in twice as many tiles of 128).
+  if (a.M > 128 && cdiv(a.M, 256) * cdiv(a.V, 256) > 128) return run_mxfp4_many<T, 256>(a, s);
+  if (a.M > 48) return run_mxfp4_many<T, 128>(a, s);
   // 64 rows of W a workgroup read x half as often as 32 (4096 x 128256: 32 rows 68 us against 79, one 51 against 48), if they
   // still leave each CU a workgroup.
   const bool wide = a.M > 4 && a.V >= 64 * 256;

@@ -113,11 +113,12 @@ def _check_product(got, x, w):
 
 
 # Rows of x around the borders of the tiles (16, 32, 48; 128; 256), rows of W around 32, 64 and 256 (and 16384, from where a workgroup
-# takes 64), K with whole and part steps of 256, one and several runs of 8192, scales' rows at any alignment.
+# takes 64), more and fewer than 128 tiles of 256 x 256, K with whole and part steps of 256, one and several runs of 8192, scales' rows at any alignment.
 @pytest.mark.parametrize("M,H,V", [
     (1, 32, 1), (1, 32, 5), (1, 256, 32), (2, 64, 33), (16, 96, 31), (17, 288, 100), (16, 1024, 1000), (32, 4096, 65), (33, 800, 63), (48, 2080, 130), (5, 8192, 66),
     (5, 8224, 66), (3, 16672, 40), (48, 20480, 33), (1, 1024, 16385), (5, 96, 16384), (20, 288, 16400), (40, 544, 16390), (48, 768, 16448), (49, 32, 7), (64, 4096, 257),
-    (65, 256, 256), (100, 288, 255), (128, 512, 300), (129, 32, 515), (129, 2048, 64), (256, 96, 257), (257, 1056, 300), (300, 4096, 513), (600, 160, 900), (1, 1 << 20, 3), (60, 1 << 20, 2)])
+    (65, 256, 256), (100, 288, 255), (128, 512, 300), (129, 32, 515), (129, 2048, 64), (256, 96, 257), (257, 1056, 300), (300, 4096, 513), (600, 160, 900), (1, 1 << 20, 3), (60, 1 << 20, 2),
+    (129, 288, 33000), (300, 96, 16500), (700, 1056, 11100), (1300, 32, 6000)])
 @pytest.mark.parametrize("dtype", list(DT))
 def test_product(lce, M, H, V, dtype):
     least = 112 if dtype == "fp16" else 118  # so that no sum leaves its range
