@@ -93,7 +93,8 @@ __device__ __forceinline__ int sample_cell(float z, float top, double rate) {
 // The larger of two, and NaN if one is.
 __device__ __forceinline__ float max_or_nan(float a, float b) { return (a >= b || a != a) ? a : b; }
 
-// A workgroup for each part (64 groups): eight lanes a group, REP pieces of 8 logits each.
+// A workgroup for each part (64 groups): eight lanes a group, REP pieces of 8 logits each. 256 x 152064 in fp32, an eighth of the rows with
+// tables and another with sums: 38 us (156 MB, 4.1 TB/s); one row of 128256 in bf16 3.4.
 template <typename T, int REP, RowEnd END>
 __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleArgs a) {
   constexpr int kGroup = 64 * REP, kRounds = kPartGroups / 32;
@@ -320,6 +321,10 @@ __device__ __forceinline__ SampleFound sample_find(SampleLds& s, uint32_t count,
 __device__ __forceinline__ int sample_shift(uint32_t span) { return span < (uint32_t)kSampleBins ? 0 : 21 - __builtin_clz(span); }
 static_assert(kSampleBins == 1 << 11, "sample_shift");
 
+// A workgroup a row. What a row waits for is its chain of searches, a barrier or two and a read of cold code each: the largest logit 3.4 us,
+// top-k 50 with top-p 17, the whole distribution 11, top-p alone 29 (128256 logits in bf16); 256 rows of 152064 with settings of their own 47,
+// the slowest of them. (Each search in one place and loops over logits rolled up: 40 KB of code; 125 KB unrolled took 30 us
+// for top-k and 70 for the 256 rows.)
 template <typename T, int REP, RowEnd END>
 __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const SampleArgs a) {
   using Key = SampleKey<T>;
