@@ -583,9 +583,15 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
       sample_clear(s);
       each([&](uint32_t key, float z, uint32_t at) {
         if (key < lo || key > hi || rank(key, at) < cut) return;
-        atomicAdd(&s.count[(hi - key) >> shift], 1u);
+        // Lanes with the first one's logit add as one: many equal logits would queue up at their bin (128256 of them 640 us).
+        const uint64_t same = __ballot(key == (uint32_t)__builtin_amdgcn_readfirstlane((int)key));
+        const bool alike = (same >> (tid & 63)) & 1;
+        const uint32_t first_of = __builtin_amdgcn_mbcnt_hi((uint32_t)(same >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)same, 0));
+        if (alike && first_of != 0) return;
+        const uint32_t times = alike ? (uint32_t)__popcll(same) : 1u;
+        atomicAdd(&s.count[(hi - key) >> shift], times);
         if (weighed) {
-          const uint64_t w = fixed(weight(z));
+          const uint64_t w = fixed(weight(z)) * times;
           if (w != 0) atomicAdd(&s.weight[(hi - key) >> shift], (unsigned long long)w);
         }
       });

@@ -45,12 +45,13 @@ def test_no_scratch_memory(report):
 
 
 def test_waves(report):
-    """Two workgroups of the product's kernel for few rows a CU, one of that for many (eight waves), one of a row's sampling."""
+    """Two workgroups of the product's kernel for few rows a CU, one of that for many (eight waves, or four in the smaller tile), one of a
+    row's sampling."""
     kernels, _ = report
     for n, use in _of(kernels, "mxfp4_few_kernel").items():
         assert use["Occupancy"] >= 2 and use["LDS Size"] <= 80 * 1024, (n, use)
     for n, use in _of(kernels, "mxfp4_many_kernel").items():
-        assert use["Occupancy"] >= 2, (n, use)
+        assert use["Occupancy"] >= (2 if n.count("Li256ELi8E") else 1), (n, use)
     for n, use in _of(kernels, "sample_row_kernel").items():
         assert use["Occupancy"] >= 4 and use["LDS Size"] <= 160 * 1024, (n, use)
 
