@@ -13,7 +13,7 @@ import math
 import torch
 
 from . import ops
-from .lce import DTYPES, LCEError, load_library
+from .lce import DTYPES, LCEError, _differentiated, load_library
 from .ops import _check_unfollowed, _pitch, _space, _upstream, _written
 
 EXPORTED = ("lce_embedding_forward", "lce_embedding_workspace_size", "lce_embedding_backward", "lce_mxfp4_quantize",
@@ -77,6 +77,26 @@ def _given(t, shape, dtype, dev, what: str):
     _check_unfollowed(t, what)
     _written([t])
     return t
+
+
+class _Undifferentiated(torch.autograd.Function):
+    """What a call gives for tensors that autograd follows: differentiating it raises, instead of finding constants."""
+
+    @staticmethod
+    def forward(ctx, call, *followed):
+        return call()
+
+    @staticmethod
+    def backward(ctx, *grads):
+        raise RuntimeError("the 4-bit product and sampling are not differentiable: detach() their input to use them as constants")
+
+    @staticmethod
+    def jvp(ctx, *tangents):
+        _Undifferentiated.backward(ctx)
+
+
+def _followed(t) -> bool:
+    return (t.requires_grad or getattr(torch.autograd.forward_ad, "_current_level", 0) >= 0) and _differentiated([t])
 
 
 # ---- embedding -----------------------------------------------------------------------------------
@@ -263,8 +283,13 @@ def mxfp4_matmul(codes, scales, weight_codes, weight_scales, dtype=torch.bfloat1
 def mxfp4_linear(hidden, weight_codes, weight_scales, out=None):
     """hidden [..., H], quantised here, times a weight in 4 bits: [..., V] of hidden's type (an output layer's logits).
 
-    Not differentiable: training keeps the weight in its own type (linear_cross_entropy).
+    Not differentiable: training keeps the weight in its own type (linear_cross_entropy). Of a hidden that autograd follows the
+    result raises if it is differentiated.
     """
+    if _followed(hidden):
+        if out is not None:
+            raise ValueError("hidden requires a gradient, and this call is not differentiable: give it detached, or call under torch.no_grad()")
+        return _Undifferentiated.apply(lambda: mxfp4_linear(hidden.detach(), weight_codes, weight_scales), hidden)
     codes, scales = mxfp4_quantize(hidden)
     return mxfp4_matmul(codes, scales, weight_codes, weight_scales, hidden.dtype, out)
 
@@ -294,8 +319,11 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, ret
     of at least that share of the largest one's probability. The kept ones, in the order of the vocabulary, divide up [0, 1) by their probabilities,
     and the token is the one whose part holds the row's number. Each setting is a number, or a tensor with one for each row (fp32; top_k:
     int32). logprobs (fp32) are the logs of the tokens' probabilities among the kept ones. A row with a NaN, or with
-    nothing above -inf, gives -1. Not differentiable.
+    nothing above -inf, gives -1. Not differentiable: the logprobs of logits that autograd follows raise if they are differentiated.
     """
+    if return_logprobs and _followed(logits):
+        plain = logits.detach()
+        return _Undifferentiated.apply(lambda: sample(plain, uniforms, temperature, top_k, top_p, min_p, True, workspace), logits)
     dev = _device_rows(logits, "logits")
     V = logits.shape[-1] if logits.dim() else 0
     if V < 1:

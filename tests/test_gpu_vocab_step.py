@@ -130,3 +130,57 @@ def test_answers_in_a_graph(lce):
         tokens.copy_(out)
         got.append(out.tolist())
     assert got == want and len(set(map(tuple, got))) > 1
+
+
+def test_what_has_no_gradient_says_so(lce):
+    """Logits of the 4-bit product and log-probabilities of drawn tokens are not constants to a gradient: asking for it raises."""
+    hidden = torch.randn((3, 64), device="cuda", requires_grad=True)
+    codes, scales = lce.mxfp4_quantize(torch.randn((40, 64), device="cuda"))
+    u = torch.rand(3, device="cuda")
+    logits = lce.mxfp4_linear(hidden, codes, scales)
+    assert torch.equal(logits, lce.mxfp4_linear(hidden.detach(), codes, scales))
+    tokens, logs = lce.sample(logits, u, top_k=5, return_logprobs=True)
+    assert not tokens.requires_grad and torch.equal(tokens, lce.sample(logits.detach(), u, top_k=5))
+    for value in (logits, logs):
+        with pytest.raises(RuntimeError, match="not differentiable"):
+            value.sum().backward()
+    with pytest.raises(ValueError):
+        lce.mxfp4_linear(hidden, codes, scales, out=torch.empty((3, 40), device="cuda"))
+    with torch.no_grad():
+        assert not lce.mxfp4_linear(hidden, codes, scales).requires_grad
+    assert not lce.sample(logits, u).requires_grad
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(hidden.detach(), torch.ones_like(hidden))
+        with pytest.raises(RuntimeError):
+            lce.mxfp4_linear(dual, codes, scales)
+
+
+def test_training_in_a_graph(lce):
+    """The embedding's lookup and gradient captured together, replayed on tokens and upstream gradients changed in place."""
+    V, N, H = 500, 3000, 264
+    weight = torch.randn((V, H), device="cuda").to(torch.bfloat16).requires_grad_()
+    tokens, dy = torch.randint(0, V, (N,), device="cuda"), torch.randn((N, H), device="cuda").to(torch.bfloat16)
+
+    def step():
+        out = lce.embedding(tokens, weight, 2.0, 7)
+        return (out.detach(), *torch.autograd.grad(out, weight, dy))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = step()
+    for k in range(4):
+        tokens.copy_((tokens * 3 + k) % V)
+        dy.mul_(-0.5)
+        want = [t.clone() for t in step()]
+        for t in outs:
+            t.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want)), k
