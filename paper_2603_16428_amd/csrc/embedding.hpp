@@ -84,8 +84,7 @@ __device__ __forceinline__ void wave_lds_order() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Exclusive prefix sum over the workgroup's threads, in their order. Two barriers: one before the first use of lds's
-// other readers ends it, one inside.
+// Exclusive prefix sum over the workgroup's threads, in their order. (The caller's barriers keep one use of lds from the next.)
 __device__ __forceinline__ uint32_t sort_scan(uint32_t v, uint32_t* lds) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t sum = v;

@@ -199,7 +199,7 @@ constexpr int kSampleThreads = 1024, kSampleBins = 2 * kSampleThreads, kSampleLi
 
 struct SampleFound {
   int bin;  // -1: the target is not reached
-  uint32_t before, count, all;
+  uint32_t before, count;
   uint64_t weight_before, weight, weight_all;
 };
 struct SampleLds {
@@ -289,7 +289,6 @@ __device__ __forceinline__ SampleFound sample_find(SampleLds& s, uint32_t count,
   // The sums of the waves before, and of all, from 16 lanes' scan.
   const uint32_t upto_c = row_scan(s.wave_count[lane & 15]);
   const uint64_t upto_w = row_scan(s.wave_weight[lane & 15]);
-  const uint32_t all_c = lane_of(upto_c, 15);
   const uint64_t all_w = lane_of(upto_w, 15);
   if (wave > 0) {
     c += lane_of(upto_c, wave - 1);
@@ -306,13 +305,12 @@ __device__ __forceinline__ SampleFound sample_find(SampleLds& s, uint32_t count,
   for (int k = 0; k < 2; ++k) {
     const uint32_t ck = k ? c1 : c0;
     const uint64_t wk = k ? w1 : w0;
-    if (!reached(c, w) && reached(c + ck, w + wk)) s.found = {b + k, c, ck, all_c, w, wk, all_w};
+    if (!reached(c, w) && reached(c + ck, w + wk)) s.found = {b + k, c, ck, w, wk, all_w};
     c += ck;
     w += wk;
   }
   __syncthreads();
   SampleFound f = s.found;
-  f.all = all_c;
   f.weight_all = all_w;
   return f;
 }
