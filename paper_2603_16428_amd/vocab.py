@@ -319,11 +319,14 @@ def sample(logits, uniforms, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, ret
     of at least that share of the largest one's probability. The kept ones, in the order of the vocabulary, divide up [0, 1) by their probabilities,
     and the token is the one whose part holds the row's number. Each setting is a number, or a tensor with one for each row (fp32; top_k:
     int32). logprobs (fp32) are the logs of the tokens' probabilities among the kept ones. A row with a NaN, or with
-    nothing above -inf, gives -1. Not differentiable: the logprobs of logits that autograd follows raise if they are differentiated.
+    nothing above -inf, gives -1. Not differentiable: the logprobs of logits or settings that autograd follows raise if they are differentiated.
     """
-    if return_logprobs and _followed(logits):
-        plain = logits.detach()
-        return _Undifferentiated.apply(lambda: sample(plain, uniforms, temperature, top_k, top_p, min_p, True, workspace), logits)
+    if return_logprobs:
+        given = logits, temperature, top_p, min_p
+        followed = [v for v in given if isinstance(v, torch.Tensor) and _followed(v)]
+        if followed:
+            z, t, p, m = (v.detach() if isinstance(v, torch.Tensor) else v for v in given)
+            return _Undifferentiated.apply(lambda: sample(z, uniforms, t, top_k, p, m, True, workspace), *followed)
     dev = _device_rows(logits, "logits")
     V = logits.shape[-1] if logits.dim() else 0
     if V < 1:

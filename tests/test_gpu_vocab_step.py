@@ -184,3 +184,24 @@ def test_training_in_a_graph(lce):
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), k
+
+
+def test_drawn_log_probabilities_are_no_constants_to_their_settings(lce):
+    """They depend on the temperature as on the logits: of a setting that autograd follows, asking for its gradient raises too."""
+    logits, u = torch.randn((3, 200), device="cuda"), torch.rand(3, device="cuda")
+    plain = dict(temperature=torch.full((3,), 0.7, device="cuda"), top_p=torch.full((3,), 0.9, device="cuda"), min_p=torch.full((3,), 0.01, device="cuda"))
+    want = lce.sample(logits, u, **plain, return_logprobs=True)
+    for name in plain:
+        for z in (logits, logits.clone().requires_grad_()):
+            settings = plain | {name: plain[name].clone().requires_grad_()}
+            tokens, logs = lce.sample(z, u, **settings, return_logprobs=True)
+            assert torch.equal(tokens, want[0]) and torch.equal(logs, want[1]) and not tokens.requires_grad
+            with pytest.raises(RuntimeError, match="not differentiable"):
+                torch.autograd.grad(logs.sum(), settings[name])
+            assert not lce.sample(z, u, **settings).requires_grad
+            with torch.no_grad():
+                assert not lce.sample(z, u, **settings, return_logprobs=True)[1].requires_grad
+        with torch.autograd.forward_ad.dual_level():
+            dual = torch.autograd.forward_ad.make_dual(plain[name], torch.ones_like(plain[name]))
+            with pytest.raises(RuntimeError):
+                lce.sample(logits, u, **(plain | {name: dual}), return_logprobs=True)
