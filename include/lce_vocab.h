@@ -81,8 +81,8 @@ lce_status_t lce_mxfp4_matmul(const void* x_codes, const void* x_scales, int64_t
  * token = the first kept v for which the sum of kept w up to and with v, by rising v, is above u times the sum of all kept.
  * A temperature that is not above 0 takes the largest logit's first place (above 1e30: as 1e30). A row with a NaN, or nothing above -inf, or whose u is NaN, gives
  * -1; u below 0 counts as 0, from 1 on the last kept token comes. +inf are the largest and equal. Weights are computed in 64 bits and
- * added in integers (a 2^42nd of the largest weight, or less): a token's smaller weight counts as none, and a result does
- * not depend on the order of additions.
+ * added in integers, so that a result does not depend on the order of additions: a running sum is off by less than a 2^25th of the
+ * kept weights together (half of the finest step of u below 1), and the sum that top_p's end is found by likewise.
  *   logits      : device [N,V] of dtype, 1 <= V <= LCE_SAMPLE_MAX_V, N <= LCE_SAMPLE_MAX_N; only read.
  *   uniforms    : device fp32 [N], the random numbers u.
  *   settings    : in HOST memory, read during the call: one value for all rows, or, where the pointer is not NULL, device [N] with

@@ -1,7 +1,9 @@
 // A token for each row of logits, from a given random number: temperature, top-k, top-p, min-p.
 //
-// Weights exp((z - max) / T) are computed in 64 bits and added as 64-bit integers (fixed point: 2^-44 of the largest weight for
-// a vocabulary of 2^18, and more for smaller ones). Integer sums do not depend on their order, so counts and weights are gathered by
+// Weights exp((z - max) / T) are computed in 64 bits and added as 64-bit integers (fixed point: V logits have a unit of 2^-44 of the
+// largest weight up to 2^18, 2^-50 up to 2^12; above 2^18 the unit follows from the row's logits, 2^-53 of their sum or 2^-50). A running
+// sum is then off by less than 2^-25 of the kept weights together, half of the finest step of a number below 1: V half units, at most
+// 2^-27, V 2^-50 for the tables' own rounding, and V 2^-45.8 for weights past the tables' end. Integer sums do not depend on their order, so counts and weights are gathered by
 // LDS atomics, and everything that is looked for (the k-th largest, where top-p ends, which of several equal ones are still in,
 // the token whose running sum passes u Z) is found the same way: 2048 bins over the range in question, a prefix sum, the bin
 // where the target is reached, and again inside that bin until it is one value. Nothing is sorted.
@@ -21,6 +23,7 @@ namespace lce {
 
 constexpr int kSampleCells = 128;  // of a quarter of T: the last one's weights are 2^-46
 constexpr int kSampleParts = 64, kPartGroups = 64, kMostGroups = kSampleParts * kPartGroups;
+constexpr double kCellUnits = 0x1p49;  // of a table's weights: a part's 2^14 logits at most stay below 2^64
 
 struct SampleArgs {
   const void* logits;
@@ -159,7 +162,7 @@ __global__ __launch_bounds__(256) void sample_parts_kernel(const SampleArgs a) {
             if (set.cells) {
               const int cell = sample_cell(z, top, set.rate);
               if (cell < kSampleCells) {
-                atomicAdd(&cell_weight[cell], (unsigned long long)(uint64_t)fma(w, 0x1p44, 0.5));
+                atomicAdd(&cell_weight[cell], (unsigned long long)(uint64_t)fma(w, kCellUnits, 0.5));
                 atomicAdd(&cell_count[cell], 1u);
               }
             }
@@ -400,9 +403,24 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
     return answer(s.lowest, 0.f);
   }
 
-  const double one = __builtin_ldexp(1.0, a.bits);
+  // The unit of the weights: all of them together stay below 2^63, one below 2^51.
+  int bits = a.bits;
+  if constexpr (REP > 1) {
+    // For very many logits the worst case's unit (all are equal) is too coarse for a tail below few large ones (2^20 weights of a
+    // 2^43rd each are 2^-23 of the large one): the groups' maxima say how large the sum can be, to a factor of the groups' length.
+    uint64_t most = 0;  // 2^-20ths
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) most += (uint64_t)(sample_weight(maxima[k], top, set.rate, s.table) * (kGroup * 0x1p20)) + 1;
+    most = wave_scan(most);
+    if ((tid & 63) == 63) s.wave_weight[tid >> 6] = most;
+    __syncthreads();
+    most = lane_of(row_scan(s.wave_weight[tid & 15]), 15);
+    bits = min(50, 82 - (64 - __builtin_clzll(most)));
+  }
+  const double one = __builtin_ldexp(1.0, bits);
   // A weight in fixed point: below 2^52, so that adding 2^52 rounds it to an integer in the low bits.
-  auto fixed = [&](double w) { return __builtin_bit_cast(uint64_t, fma(w, one, 0x1p52)) - __builtin_bit_cast(uint64_t, 0x1p52); };
+  auto in_units = [](double w, double n) { return __builtin_bit_cast(uint64_t, fma(w, n, 0x1p52)) - __builtin_bit_cast(uint64_t, 0x1p52); };
+  auto fixed = [&](double w) { return in_units(w, one); };
   auto logprob = [&](uint32_t at, double sum) {
     const float z = to_f32(row[at]);
     return (float)((z == top ? 0.0 : ((double)z - (double)top) / (double)set.T) - log(sum));
@@ -636,7 +654,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
       const uint64_t w = a.cell_weight[at];
       const float of = a.part_max[i * a.parts + part];
       const int c = sample_cell(of, top, set.rate) + k % kSampleCells;
-      if (n != 0 && c < kSampleCells) f(part, c, n, (uint64_t)((double)w * 0x1p-44 * weight(of) * one + 0.5));
+      if (n != 0 && c < kSampleCells) f(part, c, n, (uint64_t)((double)w * (1.0 / kCellUnits) * weight(of) * one + 0.5));
     }
   };
   bool by_cells = set.cells, ready = false;
@@ -700,6 +718,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
   uint32_t n = inside ? min((uint32_t)(kPartGroups * kGroup), (uint32_t)a.V - lo) : (uint32_t)a.V;
   double share = fmin(chance, 1.0);
   if (inside) share = fmin(fmax((share * (double)part.weight_all - (double)part.weight_before) / (double)part.weight, 0.0), 1.0);
+  // (a part's logits, each at most its largest, may have a finer unit than the row's, and must have room in theirs)
+  constexpr double kInside = REP == 4 ? 0x1p48 : 0x1p49;
+  const double unit = REP > 1 && inside ? kInside : one;
   uint64_t target = 0, whole = part.weight_all;
   bool first = true;
 #pragma nounroll
@@ -709,7 +730,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
     auto add = [&](uint32_t key, float z, uint32_t place) {
       if (place - lo >= n || z < bound || rank(key, place) < cut || (cell >= 0 && sample_cell(z, top, set.rate) > cell)) return;
       if (set.by_least && weight(z) < (double)set.least) return;
-      const uint64_t w = fixed(sample_weight(z, of, set.rate, s.table));
+      const uint64_t w = in_units(sample_weight(z, of, set.rate, s.table), unit);
       if (w != 0) atomicAdd(&s.weight[(place - lo) >> shift], (unsigned long long)w);
     };
     if (first && !inside) each(add);

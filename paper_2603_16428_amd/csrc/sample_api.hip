@@ -66,7 +66,7 @@ lce_status_t lce_sample(const void* logits, int64_t logits_ld, int64_t N, int64_
   uint64_t* cell_weight = (uint64_t*)(sums + N * parts);
   uint32_t* cell_count = (uint32_t*)(cell_weight + N * parts * kSampleCells);
   float* part_max = (float*)(cell_count + N * parts * kSampleCells);
-  // All weights together stay below 2^63, one below 2^51.
+  // All weights together stay below 2^63, one below 2^51 (for groups of more than 64 the kernel takes it from the row).
   const int bits = std::min(50, 62 - (V > 1 ? 32 - __builtin_clz((unsigned)(V - 1)) : 0));
   const SampleArgs a{logits, logits_ld, uniforms, c.temperature, c.top_p, c.min_p, c.top_k, c.temperatures, c.top_ps, c.min_ps, c.top_ks, tokens, logprobs,
                      part_max + N * parts, part_max, sums, cell_weight, cell_count, (int)V, groups, parts, bits};

@@ -6,6 +6,7 @@ errors below 1e-9.
 """
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -243,3 +244,32 @@ def test_streams_and_graphs(lce):
         k.copy_(k.roll(1))
         want = everything(spaces[0])
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("V", [262144, 300001, 1 << 20])
+def test_many_small_weights_together(lce, V):
+    """One large logit and a tail whose weights are some 2^-43 of its own each, but count together: u times the whole falls into the token's part, to
+    2^-25 of the whole, twice that where top-p's end is looked for as well (exact sums: extended precision, whose own roundings are V 2^-64)."""
+    u = torch.tensor([0.0, 1e-8, 2e-8, 5e-8, 0.5, 1 - 2.0 ** -24], device="cuda")
+    for tail in (2.0 ** -43.05, 2.0 ** -44.05):
+        for large in (0, V // 2, V - 1):
+            z = torch.full((V,), math.log(tail), device="cuda")
+            z[large] = 0.0
+            w = np.exp(z.cpu().double().numpy()).astype(np.longdouble)
+            for settings in (dict(), dict(min_p=1e-30), dict(top_k=V - 1), dict(top_p=1 - 2.0 ** -24), dict(top_p=1 - 2.0 ** -24, min_p=1e-30)):
+                kept = w.copy()
+                if "top_k" in settings:  # all but the last of the equal ones
+                    kept[V - 1 if large != V - 1 else V - 2] = 0
+                running = np.cumsum(kept)
+                if "top_p" in settings:  # the large one and the first of the tail
+                    last = int(np.searchsorted(np.cumsum(np.delete(w, large)), settings["top_p"] * running[-1] - 1))
+                    kept[np.delete(np.arange(V), large)[last + 1:]] = 0
+                    running = np.cumsum(kept)
+                off = (2.0 ** -24 if "top_p" in settings else 2.0 ** -25) * running[-1]
+                tokens, logs = lce.sample(z.expand(len(u), V), u, **settings, return_logprobs=True)
+                for t, log, at in zip(tokens.tolist(), logs.tolist(), u.double().tolist()):
+                    case = (V, tail, large, settings, at, t)
+                    aim = np.longdouble(at) * running[-1]
+                    assert running[t] - w[t] - off <= aim <= running[t] + off, case
+                    want = float(z[t].double()) - float(np.log(running[-1]))
+                    assert abs(log - want) <= 2.0 ** -24 * 1.01 * abs(want) + off, case
