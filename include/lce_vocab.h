@@ -67,8 +67,10 @@ lce_status_t lce_mxfp4_dequantize(const void* codes, const void* scales, int64_t
 /*
  * out = X W^T for X [M,H] and W [V,H] in 4 bits, summed in fp32 and rounded once to dtype.
  *   codes, scales : as lce_mxfp4_quantize leaves them. A group whose scale byte is 255 makes the sums that it enters NaN.
- *   out           : device [M,V] of dtype. M, V >= 0 (M, V < 2^31).
+ *   out           : device [M,V] of dtype. M, V >= 0 (M, V < 2^31; for M > 128 at most LCE_MXFP4_MAX_TILES tiles of 256 x 256 values,
+ *                   for M from 49 to 128 as many of M x 256, else LCE_ERR_UNSUPPORTED).
  */
+#define LCE_MXFP4_MAX_TILES (1 << 22)
 lce_status_t lce_mxfp4_matmul(const void* x_codes, const void* x_scales, int64_t M, const void* w_codes, const void* w_scales,
                               int64_t V, int64_t H, int dtype, void* out, int64_t out_ld, void* stream);
 

@@ -32,7 +32,7 @@ lce_status_t run_mxfp4_many(MxMatmulArgs a, hipStream_t s) {
   a.tiles_m = (int)cdiv(a.M, BN);
   a.tiles_v = (int)cdiv(a.V, 256);
   const int64_t tiles = (int64_t)a.tiles_m * a.tiles_v;
-  if (tiles > (1 << 22)) return LCE_ERR_UNSUPPORTED;
+  if (tiles > LCE_MXFP4_MAX_TILES) return LCE_ERR_UNSUPPORTED;
   constexpr int kWaves = BN / 32;
   auto kernel = mxfp4_many_kernel<T, BN, kWaves>;
   constexpr int kSmem = mx_many_smem<BN>();
@@ -52,7 +52,18 @@ lce_status_t run_mxfp4_matmul(const MxMatmulArgs& a, hipStream_t s) {
   // 64 rows of W a workgroup read x half as often as 32 (4096 x 128256: 32 rows 68 us against 79, one 51 against 48), if they
   // still leave each CU a workgroup.
   const bool wide = a.M > 4 && a.V >= 64 * 256;
-  auto go = [&](auto kernel, int rows) { hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv(a.V, rows)), dim3(256), 0, s, a); };
+  // (a launch's threads are counted in 32 bits: 2^28 rows of W at a time)
+  constexpr int64_t kRowsAtOnce = int64_t(1) << 28;
+  auto go = [&](auto kernel, int rows) {
+    for (int64_t v = 0; v < a.V; v += kRowsAtOnce) {
+      MxMatmulArgs b = a;
+      b.w += v * (a.K / 2);
+      b.w_scales += v * (a.K / kMxGroup);
+      b.out = (T*)a.out + v;
+      b.V = std::min(a.V - v, kRowsAtOnce);
+      hipLaunchKernelGGL(kernel, dim3((unsigned)cdiv(b.V, rows)), dim3(256), 0, s, b);
+    }
+  };
   if (a.M <= 16) wide ? go(mxfp4_few_kernel<T, 1, 4>, 64) : go(mxfp4_few_kernel<T, 1, 2>, 32);
   else if (a.M <= 32) wide ? go(mxfp4_few_kernel<T, 2, 4>, 64) : go(mxfp4_few_kernel<T, 2, 2>, 32);
   else wide ? go(mxfp4_few_kernel<T, 3, 4>, 64) : go(mxfp4_few_kernel<T, 3, 2>, 32);

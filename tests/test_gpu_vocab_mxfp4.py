@@ -225,3 +225,19 @@ def test_streams_and_graphs(lce):
         many.add_(0.125)
         want = everything()
         torch.cuda.synchronize()
+
+
+def test_a_weight_of_more_rows_than_a_launch_has_threads(lce):
+    """2^29 rows and some, for few rows of x: the rows around the pieces' borders and the last ones are right, all others zero."""
+    V = (1 << 29) + 77
+    codes = torch.zeros((V, 16), dtype=torch.uint8, device="cuda")
+    scales = torch.full((V, 1), 127, dtype=torch.uint8, device="cuda")
+    at = torch.cat([torch.arange(k - 40, k + 40) for k in (40, 1 << 28, 1 << 29)] + [torch.arange(V - 3, V)])
+    w = _packed(len(at), 32, 10)
+    codes[at.cuda()], scales[at.cuda()] = w[0].cuda(), w[1].cuda()
+    for M in (1, 9):
+        x = _packed(M, 32, 11)
+        out = lce.mxfp4_matmul(*(t.cuda() for t in x), codes, scales)
+        _check_product(out[:, at.cuda()], x, w)
+        out[:, at.cuda()] = 0
+        assert not bool(out.any())

@@ -137,3 +137,17 @@ def test_binding_refuses():
                  lambda: lce.mxfp4_dequantize(c, s), lambda: lce.mxfp4_matmul(c, s, c, s), lambda: lce.mxfp4_linear(x, c, s), lambda: lce.sample(x, torch.zeros(2))):
         with pytest.raises(ValueError):
             call()
+
+
+def test_mxfp4_matmul_of_too_many_tiles(lib):
+    """The header's limit, on both sides of 128 rows (at the limit itself a launch is tried, which needs a GPU)."""
+    text = open(os.path.join(ROOT, "include", "lce_vocab.h")).read()
+    most = eval(re.search(r"LCE_MXFP4_MAX_TILES \((.*)\)", text).group(1))
+    far = [(1 << 50) + k * (1 << 45) for k in range(5)]
+
+    def call(M, V):
+        return lib.lce_mxfp4_matmul(far[0], far[1], M, far[2], far[3], V, 32, BF16, far[4], V, None)
+
+    for M, V in ((49, 256 * most + 1), (128, 256 * most + 1), (129, 256 * most + 1), (256 * most + 1, 1), (256 * 2048 + 1, 256 * (most // 2048)),
+                 (256 * 2048, 256 * (most // 2048) + 1)):
+        assert call(M, V) == UNSUPPORTED, (M, V)
