@@ -660,8 +660,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_row_kernel(const Sample
   bool by_cells = set.cells, ready = false;
   const double of_row = sum;
 #pragma nounroll
-  for (int what = set.whole() ? 3 : 0; what < 3; ++what) {  // top-k, then top-p
-    const bool wanted = what == 0 ? set.by_k : what == 1 && set.by_p;
+  for (int what = set.whole() ? 2 : 0; what < 2; ++what) {  // top-k, then top-p
+    const bool wanted = what == 0 ? set.by_k : set.by_p;
     if (!wanted && (by_cells || ready)) continue;
     const uint32_t count = what == 0 ? (uint32_t)set.k : ~0u;
     const uint64_t target = what == 0 ? ~0ull : share_of(sum * one);
