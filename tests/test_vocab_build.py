@@ -73,3 +73,26 @@ def test_products_wait_for_their_own_step_alone(report):
         first = loop.index("v_mfma_scale")
         waits = [int(n) for n in re.findall(r"vmcnt\((\d+)\)", loop[:first])]
         assert waits and max(waits) > 0, (name, waits)
+
+
+def test_neither_half_of_the_loop_waits_for_all_loads(report):
+    """The same for every wait in both halves of the loop (two steps, each with the loads of the one after it); only the last, shorter step, behind
+    it, waits for all that is on the way."""
+    _, text = report
+    names = re.findall(r"^(_ZN3lce16mxfp4_few_kernel\S+):", text, re.M)
+    assert names
+    for name in names:
+        body = text[text.index(name + ":"):]
+        body = body[:body.index(".Lfunc_end")]
+        blocks = [b for b in re.split(r"^\.LBB\w+:", body, flags=re.M) if b.count("v_mfma_scale") >= 4 and "buffer_load_dwordx4" in b]
+        waits = [[int(n) for n in re.findall(r"vmcnt\((\d+)\)", b)] for b in blocks]
+        assert len(blocks) == 3 and all(w and min(w) > 0 for w in waits[:2]), (name, waits)
+
+
+def test_a_row_of_logits_spills_no_more_than_is_known(report):
+    """The row's kernel of sampling has all its paths in 128 registers of 1024 threads, and spills: 200 bytes a lane in 16 bits, 268 in fp32 (up to
+    2^18 logits), 300 at most."""
+    kernels, _ = report
+    for n, use in _of(kernels, "sample_row_kernel").items():
+        usual = "Li1ELNS_6RowEndE1E" in n
+        assert use["ScratchSize"] <= ((272 if "kernelIfLi" in n else 204) if usual else 304), (n, use)
