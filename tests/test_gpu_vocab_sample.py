@@ -273,3 +273,11 @@ def test_many_small_weights_together(lce, V):
                     assert running[t] - w[t] - off <= aim <= running[t] + off, case
                     want = float(z[t].double()) - float(np.log(running[-1]))
                     assert abs(log - want) <= 2.0 ** -24 * 1.01 * abs(want) + off, case
+
+
+@pytest.mark.parametrize("V", [9000, 100003, 150016])
+def test_all_three_settings_beyond_the_groups(lce, V):
+    """A top-k above the number of groups (V / 64) with top-p and min-p, peaked and nearly flat: neither tables nor a bound by the groups."""
+    for dtype in DT:
+        for sharp in (1.5, 0.05):
+            _check(lce, *_logits(3, V, dtype, sharp, 5), top_k=3000, top_p=0.9, min_p=0.05)
