@@ -180,8 +180,8 @@ struct MxScaleRun {
 // Few rows of x (up to 16 MT): W is read once, straight into registers, and nothing else takes long. A workgroup has 16 NV rows
 // of W; its four waves take the steps of K in turn, the next one requested before the current one's products, and add up at
 // the end. x comes from L2: 16 NV rows of W for each read of it. Lane quarter q takes groups q and 4 + q of a step's eight.
-// Bound by HBM for one row (4096 x 128256: 47 us, 279 MB, 5.9 TB/s), for more by x's way from L2 as well (48 rows 77 us, 48 rows of
-// 12288 x 32768 56 us: 3.9 TB/s of W, as much again of x).
+// Bound by HBM for one row (4096 x 128256: 47 us, 279 MB, 5.9 TB/s), for more by x's way from L2 as well (48 rows 77 us; 48 rows of
+// 12288 x 32768 56 us: 3.9 TB/s of W, and 171 MB of L2 hits, mostly x: the waves take different steps, so a workgroup shares nothing of it).
 template <typename T, int MT, int NV>
 __global__ __launch_bounds__(256, 2) void mxfp4_few_kernel(const MxMatmulArgs a) {
   constexpr int kRowsW = 16 * NV, kRowsX = 16 * MT, kPitch = kRowsW + 4, kWaves = 4, kTiles = NV > MT ? NV : MT;
@@ -308,9 +308,10 @@ __global__ __launch_bounds__(256, 2) void mxfp4_few_kernel(const MxMatmulArgs a)
 // waves, 64 x 128; four of 128 x 128 read less from LDS but have nothing to run under their waits, 924 us against 733 for
 // 2048 x 3584 x 152064; BN 128: four waves, 128 x 64, 89 us against 91 with eight for 128 x 4096 x 128256). A step is 256
 // values of K, 128 bytes of a row: whole cache lines, LDS-DMA loads of 8 rows each into one of two slots. The 16-byte
-// pieces of LDS row r are permuted by r % 8, so that a fragment's 16 rows lie in distinct banks. The scales go through
-// registers, since their rows may begin at any byte. Bound by LDS: what a step's fragments read and its loads write takes as
-// long as its products at the full rate. 2048 x 3584 x 152064: 3.0 PFLOP/s, 4096 x 8192 x 32000: 3.5.
+// pieces of LDS row r are permuted by r % 8: a fragment's rows r and r + 8 still share their banks, all others differ (half of a read's 8
+// cycles). The scales go through registers, since their rows may begin at any byte. 2048 x 3584 x 152064: 3.0 PFLOP/s, 4096 x 8192 x 32000:
+// 3.5. Bound by waiting: the MFMAs are busy 33% of the time and LDS 29% (counters, first shape); a step's loads are one step ahead and
+// all waited for, its fragments are all read behind that barrier, and a tile's first loads and its result have nothing beside them.
 template <typename T, int BN, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void mxfp4_many_kernel(const MxMatmulArgs a) {
   constexpr int kBM = 256, kWaves = WAVES, kWavesV = WAVES / 2, kI = kBM / kWavesV / 16, kJ = BN / 32, kThreads = 64 * WAVES;

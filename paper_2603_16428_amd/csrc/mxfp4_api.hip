@@ -44,7 +44,9 @@ lce_status_t run_mxfp4_many(MxMatmulArgs a, hipStream_t s) {
 template <typename T>
 lce_status_t run_mxfp4_matmul(const MxMatmulArgs& a, hipStream_t s) {
   // Few rows read W straight into registers. From 49 on the tile of 128 is the faster (4096 x 128256: 48 rows 76 us, 64 rows
-  // 89 us so and 86 in the tile, which takes 89 for 128).
+  // 89 us so and 86 in the tile, which takes 89 for 128). The rule does not look at V, and loses where a workgroup for 256 rows of W
+  // leaves CUs idle that the kernel for few rows has work for: 48 and 49 rows take 49 and 88 us for 12288 x 32768, 13 and 47 for 8192 x 4096, 9 and
+  // 26 for 4096 x 2048. (Smaller tiles of W, or K split over workgroups, are what is missing there.)
   // More rows than that take the tile of 256 (256 rows: 107 us against 152, 2048: 686 against 1168) where it leaves no more than half of
   // the 256 CUs without one (2048 x 1024 x 2048: 14 us, 11 in twice as many tiles of 128).
   if (a.M > 128 && cdiv(a.M, 256) * cdiv(a.V, 256) > 128) return run_mxfp4_many<T, 256>(a, s);

@@ -322,7 +322,8 @@ __device__ __forceinline__ SampleFound sample_find(SampleLds& s, uint32_t count,
 __device__ __forceinline__ int sample_shift(uint32_t span) { return span < (uint32_t)kSampleBins ? 0 : 21 - __builtin_clz(span); }
 static_assert(kSampleBins == 1 << 11, "sample_shift");
 
-// A workgroup a row. What a row waits for is its chain of searches, a barrier or two and a read of cold code each: the largest logit 3.4 us,
+// A workgroup a row. All paths share the 128 registers that 1024 threads leave a lane, and 200 to 300 bytes of each lane's are spilled; how
+// much of a row's time that is, beside its chain of searches (a barrier or two and a read of cold code each), was not measured. The largest logit 3.4 us,
 // top-k 50 with top-p 17, the whole distribution 11, top-p alone 29 (128256 logits in bf16); 256 rows of 152064 with settings of their own 47,
 // the slowest of them. (Each search in one place and loops over logits rolled up: 40 KB of code; 125 KB unrolled took 30 us
 // for top-k and 70 for the 256 rows.)

@@ -119,8 +119,8 @@ def _check_scale(scale):
 def embedding_forward(tokens, weight, scale: float = 1.0, out=None):
     """scale * weight[tokens]: [..., H] of weight's type, each value rounded once.
 
-    tokens [...] (int64 or int32), weight [V, H] with consecutive values in a row. A token outside [0, V) gives a row of NaN.
-    Not differentiable: see embedding.
+    tokens [...] (int64 or int32, contiguous), weight [V, H] with consecutive values in a row. A token outside [0, V) gives a row
+    of NaN. Not differentiable, in forward mode either: see embedding.
     """
     dev = _device_rows(weight, "weight")
     if weight.dim() != 2 or weight.shape[0] < 1 or weight.shape[1] < 1:
@@ -149,7 +149,8 @@ def embedding_backward(grad, tokens, num_embeddings: int, scale: float = 1.0, pa
 
     Sums are fp32 in an order that the tokens fix, rounded once. grad_weight may be given; with accumulate the sums are added
     to the values there (that of linear_cross_entropy where the output layer has the same weight), and only the rows
-    that tokens name are read and written. Rows of padding_idx, and of tokens outside the matrix, count for nothing.
+    that tokens name are read and written. Rows of padding_idx, and of tokens outside the matrix, count for nothing. tokens are
+    contiguous. Not differentiable, in forward mode either.
     """
     dev = _device_rows(grad, "grad")
     size = _check_tokens(tokens, dev)
@@ -204,7 +205,11 @@ class Embedding(torch.autograd.Function):
 
 
 def embedding(tokens, weight, scale: float = 1.0, padding_idx: int | None = None):
-    """scale * weight[tokens]. Differentiable (once) with respect to weight; rows of padding_idx get no gradient."""
+    """scale * weight[tokens] for contiguous tokens. Differentiable (once) with respect to weight; rows of padding_idx get no gradient.
+
+    The gradient is a tensor of weight's size: where weight is an output layer's too, autograd adds up two of them. (A backward
+    written by hand adds the second in place: embedding_backward with accumulate.)
+    """
     return Embedding.apply(tokens, weight, scale, padding_idx)
 
 
